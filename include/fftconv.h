@@ -8,8 +8,8 @@
  * small 1-D / 2-D real FFTs of Section 5 as stand-alone calls.
  *
  * Conventions common to every call
- *  - All tensor pointers are DEVICE pointers to dense, row-major fp32 memory owned by
- *    the caller ("BDHW", innermost = image row, Section 3.1).  Inputs are never
+ *  - All tensor pointers are DEVICE pointers to dense, row-major fp32 memory (the operators at
+ *    the end also take bf16 and fp16) owned by the caller ("BDHW", innermost = image row, Section 3.1).  Inputs are never
  *    modified; outputs are fully overwritten (except fft_conv_accgrad with
  *    accumulate != 0).  Input and output ranges must not overlap.
  *  - Work is enqueued on the handle's stream and the call returns without waiting for
@@ -370,6 +370,64 @@ int fft_conv_backward(fftconv_handle hd, const float *gy, float *gx, float *gw,
 int fftconv_set_profiling(fftconv_handle h, int enabled);
 int fftconv_last_kernel_ms(fftconv_handle h, float *ms_out, int capacity, int *count);
 const char *fftconv_last_kernel_label(fftconv_handle h, int i);
+
+/*
+ * The operators around the convolution passes in a training step on discrete inputs: tokens to
+ * planes (embedding), features to a loss over many classes (xent), and the norm that bounds the step
+ * (grad).  Their operands are fp32, bf16 or fp16 (dtype: FFTCONV_F32, ...), all tensors of a call of
+ * one type unless said otherwise; sums, softmax statistics, losses and norms are fp32 or wider.
+ *  - Tokens and targets are int32 or int64 (token_bits 32 or 64).  A value outside 0 .. V-1 stands
+ *    for no token: its row of an embedding is zero, its loss is zero, it takes no part in any
+ *    gradient, and what the row's features hold (NaN too) is not read.
+ *  - T = 0: features are rows [N, D].  T > 0: they are planes [N / T, D, T], the BDHW tensors of
+ *    the passes with T = h * w positions and D planes; tokens and losses are [N / T, T] then.
+ *  - Rows, features, classes: up to 2^30 each, else FFTCONV_UNSUPPORTED.  N = 0 is a no-op, except
+ *    that a gradient which is not accumulated becomes zero.
+ *  - Results do not depend on the order in which workgroups run: the same call gives the same bits.
+ *  - The calls run on the handle's device, whichever is current.  `ws`: 16-byte aligned device scratch
+ *    of at least the size function's bytes, or NULL for the handle's own buffer.  Under graph capture a
+ *    workspace must be passed (else FFTCONV_WORKSPACE_TOO_SMALL): the handle's buffer may move later.
+ *    Two graphs that may run at the same time need two workspaces.
+ */
+enum { FFTCONV_F32 = 0, FFTCONV_BF16 = 1, FFTCONV_F16 = 2 };
+
+/* y[n] = scale * table[tokens[n]]: table[V, D] -> y, rows or planes. */
+int fftconv_embedding_fprop(fftconv_handle hd, int dtype, const void *table, const void *tokens, int token_bits, void *y,
+                            long N, int D, int V, int T, float scale);
+/* gtable[v] = scale * sum of gy[n] over the n with tokens[n] = v (+ previous gtable if accumulate != 0, which
+ * then leaves the rows that no token names as they are).  The sum is formed in fp32 in the order of n. */
+size_t fftconv_embedding_workspace_bytes(int dtype, long N, int D, int V, int T);
+int fftconv_embedding_accgrad(fftconv_handle hd, int dtype, const void *gy, const void *tokens, int token_bits, void *gtable,
+                              long N, int D, int V, int T, float scale, int accumulate, void *ws, size_t ws_bytes);
+
+/*
+ * Softmax cross entropy of a linear classifier, x (rows or planes) and wt[V, D], without its scores
+ * z = x wt^T in memory: lse[n] = log sum_v exp z[n, v] and loss[n] = lse[n] - z[n, targets[n]], fp32.
+ * backward takes the lse that fprop left for the same x, wt and targets, and gives gx (x's shape) and gw[V, D]
+ * of the loss  scale * sum_n gloss[n] loss[n]  (gloss NULL: all ones), divided by the number of rows that
+ * have a target if mean != 0 (no row: all gradients zero).  gw is added to if accumulate != 0;
+ * either of gx, gw may be NULL.  The gradient of the scores is rounded once to the operands' type (fp32: not rounded)
+ * before it meets wt and x.  pass: FFTCONV_FPROP, or FFTCONV_BPROP for the backward call.
+ */
+size_t fftconv_xent_workspace_bytes(int pass, int dtype, long N, int D, int V);
+int fftconv_xent_fprop(fftconv_handle hd, int dtype, const void *x, const void *wt, const void *targets, int token_bits,
+                       float *loss, float *lse, long N, int D, int V, int T, void *ws, size_t ws_bytes);
+int fftconv_xent_backward(fftconv_handle hd, int dtype, const void *x, const void *wt, const void *targets, int token_bits,
+                          const float *lse, const float *gloss, void *gx, void *gw, long N, int D, int V, int T,
+                          float scale, int mean, int accumulate, void *ws, size_t ws_bytes);
+
+/*
+ * The 2-norm of `count` tensors taken together (host arrays of device pointers, element counts and types;
+ * read during the call only), into norm[0] on the device.  grad_clip also writes
+ * out[i] = grads[i] * min(1, max_norm / norm); out[i] has the type of grads[i], and may be grads[i] itself.  A
+ * norm that is infinite or not a number leaves the values as they are.  Outputs that overlap each other, or
+ * another tensor's input, and a max_norm that is not positive and finite give FFTCONV_INVALID_ARG.
+ */
+size_t fftconv_grad_workspace_bytes(int count, const long *sizes);
+int fftconv_grad_norm(fftconv_handle hd, int count, const void *const *grads, const long *sizes, const int *dtypes, float *norm,
+                      void *ws, size_t ws_bytes);
+int fftconv_grad_clip(fftconv_handle hd, int count, const void *const *grads, const long *sizes, const int *dtypes,
+                      void *const *out, float max_norm, float *norm, void *ws, size_t ws_bytes);
 
 #ifdef __cplusplus
 }

@@ -32,6 +32,9 @@ SYMBOLS = [
     "fftconv_saved_bytes_padded", "fftconv_backward_workspace_bytes_padded",
     "fft_conv_fprop_save_padded", "fft_conv_backward_padded",
     "fftconv_static_scratch_bytes", "fft_conv_fprop_static", "fftconv_describe_plan",
+    "fftconv_embedding_fprop", "fftconv_embedding_accgrad", "fftconv_embedding_workspace_bytes",
+    "fftconv_xent_fprop", "fftconv_xent_backward", "fftconv_xent_workspace_bytes",
+    "fftconv_grad_norm", "fftconv_grad_clip", "fftconv_grad_workspace_bytes",
 ]
 
 
@@ -122,6 +125,19 @@ def load_library():
     lib.fftconv_static_scratch_bytes.argtypes = []
     lib.fftconv_static_scratch_bytes.restype = sz
     lib.fft_conv_fprop_static.argtypes = [vp, vp, vp, vp] + [i] * 7
+    lib.fftconv_embedding_fprop.argtypes = [vp, i, vp, vp, i, vp, l, i, i, i, f]
+    lib.fftconv_embedding_workspace_bytes.argtypes = [i, l, i, i, i]
+    lib.fftconv_embedding_workspace_bytes.restype = sz
+    lib.fftconv_embedding_accgrad.argtypes = [vp, i, vp, vp, i, vp, l, i, i, i, f, i, vp, sz]
+    lib.fftconv_xent_workspace_bytes.argtypes = [i, i, l, i, i]
+    lib.fftconv_xent_workspace_bytes.restype = sz
+    lib.fftconv_xent_fprop.argtypes = [vp, i, vp, vp, vp, i, vp, vp, l, i, i, i, vp, sz]
+    lib.fftconv_xent_backward.argtypes = [vp, i, vp, vp, vp, i, vp, vp, vp, vp, l, i, i, i, f, i, i, vp, sz]
+    lib.fftconv_grad_workspace_bytes.argtypes = [i, vp]
+    lib.fftconv_grad_workspace_bytes.restype = sz
+    lib.fftconv_grad_norm.argtypes = [vp, i, vp, vp, vp, vp, vp, sz]
+    lib.fftconv_grad_clip.argtypes = [vp, i, vp, vp, vp, vp, f, vp, vp, sz]
+    _types.update({_torch.float32: F32, _torch.bfloat16: BF16, _torch.float16: F16})
     _lib = lib
     return lib
 
@@ -139,6 +155,8 @@ def _dev_f32(t, name):
 
 
 FPROP, BPROP, ACCGRAD = 0, 1, 2
+F32, BF16, F16 = 0, 1, 2
+_types = {}           # torch type -> F32, BF16, F16; filled by load_library()
 
 PLAN_FIELDS = ("Nr Nc tiled rect bins tile_log2 planesA planesB planesC hA wA hB wB hC wC M N K conjA conjB "
                "a_rs a_cs b_rs b_cs c_rs c_cs offA offB offC total bytesA").split()
@@ -638,3 +656,199 @@ class Handle:
         self._sync_stream()
         _check(self._lib.fft_c2r_2d(self._h, _dev_f32(X, "in"), _dev_f32(out, "out"), B, n, h_out, w_out), "fft_c2r_2d")
         return out
+
+    # ---- embedding, loss and gradient norm ------------------------------------------------
+    # (methods without a counterpart in the convolution passes: their operands may be float32, bfloat16
+    # or float16, and they run on the handle's device and that device's current stream)
+    def _device_stream(self):
+        if _forked:
+            torch.cuda.init()          # refuses a process that was forked after the device's initialisation
+        try:
+            s = torch._C._cuda_getCurrentRawStream(self.device)
+        except AttributeError:         # (not part of torch's interface)
+            s = torch.cuda.current_stream(self.device).cuda_stream
+        if s != self._stream:
+            _check(self._lib.fftconv_set_stream(self._h, ctypes.c_void_p(s)), "fftconv_set_stream")
+            self._stream = s
+
+    def _on_device(self, t, name):
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous()):
+            raise FFTConvError(f"{name} must be a contiguous tensor in device memory")
+        if t.get_device() != self.device:
+            raise FFTConvError(f"{name} is on device {t.get_device()}, the handle on {self.device}")
+        return t.data_ptr()
+
+    def _typed(self, t, dtype, shape, name):
+        p = self._on_device(t, name)
+        if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+            raise FFTConvError(f"{name} must be {dtype} of shape {tuple(shape)}, not {t.dtype} of {tuple(t.shape)}")
+        return p
+
+    def _operand(self, t, name):
+        p = self._on_device(t, name)
+        k = _types.get(t.dtype)
+        if k is None:
+            raise FFTConvError(f"{name} must be float32, bfloat16 or float16, not {t.dtype}")
+        return p, k
+
+    def _tokens(self, t, name):
+        p = self._on_device(t, name)
+        if t.dtype == torch.int64:
+            return p, 64
+        if t.dtype == torch.int32:
+            return p, 32
+        raise FFTConvError(f"{name} must be int32 or int64, not {t.dtype}")
+
+    def _scratch(self, ws):
+        if ws is None:
+            return None, 0
+        return self._on_device(ws, "ws"), ws.numel() * ws.element_size()
+
+    @staticmethod
+    def _feature_shape(tokens, D, planes, name):
+        """(shape of features over these tokens, positions in a sample or 0)"""
+        s = tuple(tokens.shape)
+        if not planes:
+            return s + (D,), 0
+        if len(s) < 2:
+            raise FFTConvError(f"planes need {name} of a sample dimension and at least one position dimension")
+        T = 1
+        for n in s[1:]:
+            T *= n
+        return (s[0], D) + s[1:], T
+
+    def embedding_workspace_bytes(self, dtype, N, D, V, T=0) -> int:
+        return int(self._lib.fftconv_embedding_workspace_bytes(_types[dtype], N, D, V, T))
+
+    def embedding_fprop(self, table, tokens, scale=1.0, planes=False, y=None):
+        """scale * table[tokens]: [..., D], or with planes=True [S, D, ...] for tokens [S, ...] (what the
+        convolution passes take).  A token outside 0 .. V-1 gives zeros."""
+        p, k = self._operand(table, "table")
+        if table.dim() != 2:
+            raise FFTConvError("table must be [V, D]")
+        V, D = table.shape
+        t, bits = self._tokens(tokens, "tokens")
+        shape, T = self._feature_shape(tokens, D, planes, "tokens")
+        if y is None:
+            y = torch.empty(shape, device=table.device, dtype=table.dtype)
+            to = y.data_ptr()
+        else:
+            to = self._typed(y, table.dtype, shape, "y")
+        self._device_stream()
+        _check(self._lib.fftconv_embedding_fprop(self._h, k, p, t, bits, to, tokens.numel(), D, V, T, float(scale)),
+               "fftconv_embedding_fprop")
+        return y
+
+    def embedding_accgrad(self, gy, tokens, V, scale=1.0, planes=False, gtable=None, accumulate=False, ws=None):
+        """The gradient of embedding_fprop's table of V rows from the gradient of its result."""
+        p, k = self._operand(gy, "gy")
+        t, bits = self._tokens(tokens, "tokens")
+        if gy.dim() < (2 if planes else 1):
+            raise FFTConvError("gy and tokens disagree")
+        D = gy.shape[1 if planes else -1]
+        shape, T = self._feature_shape(tokens, D, planes, "tokens")
+        if tuple(gy.shape) != shape:
+            raise FFTConvError("gy and tokens disagree")
+        if gtable is None:
+            if accumulate:
+                raise FFTConvError("accumulate needs an existing gtable")
+            gtable = torch.empty((V, D), device=gy.device, dtype=gy.dtype)
+            to = gtable.data_ptr()
+        else:
+            to = self._typed(gtable, gy.dtype, (V, D), "gtable")
+        self._device_stream()
+        _check(self._lib.fftconv_embedding_accgrad(self._h, k, p, t, bits, to, tokens.numel(), D, V, T, float(scale),
+                                                   1 if accumulate else 0, *self._scratch(ws)), "fftconv_embedding_accgrad")
+        return gtable
+
+    def xent_workspace_bytes(self, pass_, dtype, N, D, V) -> int:
+        return int(self._lib.fftconv_xent_workspace_bytes(pass_, _types[dtype], N, D, V))
+
+    def _classifier(self, x, wt, targets, planes):
+        px, k = self._operand(x, "x")
+        pw = self._on_device(wt, "wt")
+        if wt.dim() != 2 or wt.dtype != x.dtype:
+            raise FFTConvError("wt must be [V, D] of x's type")
+        V, D = wt.shape
+        pt, bits = self._tokens(targets, "targets")
+        shape, T = self._feature_shape(targets, D, planes, "targets")
+        if tuple(x.shape) != shape:
+            raise FFTConvError("x, wt and targets disagree")
+        return (k, px, pw, pt, bits), (targets.numel(), D, V, T)
+
+    def xent_fprop(self, x, wt, targets, planes=False, loss=None, lse=None, ws=None):
+        """(loss, lse) by row, float32, of the softmax cross entropy of the scores x wt^T against `targets`:
+        x [..., D], or with planes=True [S, D, ...]; wt [V, D].  A target outside 0 .. V-1 marks a row without
+        one: its loss and lse are zero and its features are not read."""
+        args, sizes = self._classifier(x, wt, targets, planes)
+        outs = []
+        for t, name in ((loss, "loss"), (lse, "lse")):
+            if t is None:
+                t = torch.empty(targets.shape, device=x.device, dtype=torch.float32)
+                outs.append((t, t.data_ptr()))
+            else:
+                outs.append((t, self._typed(t, torch.float32, targets.shape, name)))
+        self._device_stream()
+        _check(self._lib.fftconv_xent_fprop(self._h, *args, outs[0][1], outs[1][1], *sizes, *self._scratch(ws)), "fftconv_xent_fprop")
+        return outs[0][0], outs[1][0]
+
+    def xent_backward(self, x, wt, targets, lse, gloss=None, scale=1.0, mean=False, planes=False, gx=None, gw=None,
+                      want_gx=True, want_gw=True, accumulate=False, ws=None):
+        """(gx, gw) of scale * sum(gloss * loss), gloss None for ones, divided by the number of rows that have a
+        target if `mean`; lse as xent_fprop left it.  gw is added to if `accumulate`."""
+        args, sizes = self._classifier(x, wt, targets, planes)
+        pl = self._typed(lse, torch.float32, targets.shape, "lse")
+        pg = None if gloss is None else self._typed(gloss, torch.float32, targets.shape, "gloss")
+        px = pw = None
+        if want_gx:
+            if gx is None:
+                gx = torch.empty_like(x)
+            px = self._typed(gx, x.dtype, x.shape, "gx")
+        if want_gw:
+            if gw is None:
+                if accumulate:
+                    raise FFTConvError("accumulate needs an existing gw")
+                gw = torch.empty_like(wt)
+            pw = self._typed(gw, wt.dtype, wt.shape, "gw")
+        self._device_stream()
+        _check(self._lib.fftconv_xent_backward(self._h, *args, pl, pg, px, pw, *sizes, float(scale), 1 if mean else 0,
+                                               1 if accumulate else 0, *self._scratch(ws)), "fftconv_xent_backward")
+        return gx, gw
+
+    def grad_workspace_bytes(self, grads) -> int:
+        n = len(grads)
+        return int(self._lib.fftconv_grad_workspace_bytes(n, (ctypes.c_long * n)(*[t.numel() for t in grads])))
+
+    def _tensor_list(self, grads):
+        n = len(grads)
+        got = [self._operand(t, "a gradient") for t in grads]
+        return n, (ctypes.c_void_p * n)(*[p for p, _ in got]), (ctypes.c_long * n)(*[t.numel() for t in grads]), \
+            (ctypes.c_int * n)(*[k for _, k in got])
+
+    def _norm_result(self, norm):
+        if norm is None:
+            norm = torch.empty((), device=f"cuda:{self.device}", dtype=torch.float32)
+            return norm, norm.data_ptr()
+        return norm, self._typed(norm, torch.float32, (), "norm")
+
+    def grad_norm(self, grads, norm=None, ws=None):
+        """The 2-norm of a list of tensors taken together, as a float32 tensor on the device."""
+        args = self._tensor_list(grads)
+        norm, to = self._norm_result(norm)
+        self._device_stream()
+        _check(self._lib.fftconv_grad_norm(self._h, *args, to, *self._scratch(ws)), "fftconv_grad_norm")
+        return norm
+
+    def grad_clip(self, grads, max_norm, out=None, norm=None, ws=None):
+        """Scales a list of tensors, in place or into the tensors of `out`, so that their norm taken together is at
+        most max_norm; returns the norm before that.  A norm that is not finite leaves the values as they are."""
+        args = self._tensor_list(grads)
+        to = args[1]
+        if out is not None:
+            if len(out) != len(grads):
+                raise FFTConvError("out and the gradients disagree")
+            to = (ctypes.c_void_p * len(out))(*[self._typed(o, t.dtype, t.shape, "out") for o, t in zip(out, grads)])
+        norm, pn = self._norm_result(norm)
+        self._device_stream()
+        _check(self._lib.fftconv_grad_clip(self._h, *args, to, float(max_norm), pn, *self._scratch(ws)), "fftconv_grad_clip")
+        return norm

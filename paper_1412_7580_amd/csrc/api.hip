@@ -9,14 +9,13 @@
 // each followed by the inverse transform and a crop at the origin.
 #include <cstdlib>
 #include "../../include/fftconv.h"
+#include "context.hpp"
 #include "kernels.hpp"
 
 #include <mutex>
 #include <new>
 
 using namespace fc;
-
-constexpr int kMaxKernels = 8;
 
 // Scratch for fft_conv_fprop_static, the entry point for callers that cannot allocate: the three
 // frequency-domain tensors of one fprop live in this array instead of a workspace.  Every GPU
@@ -47,22 +46,6 @@ static hipError_t static_scratch_for(int device, void **out) {
 }
 
 struct PassPlan;
-struct PlanCache;
-
-struct fftconv_ctx {
-    int device;
-    GemmSwitches sw;        // A/B switches of the contraction, read from the environment at creation
-    PlanCache *plans;       // plans of the layer shapes seen so far
-    hipStream_t stream;
-    void *ws;
-    size_t ws_bytes;
-    void *static_scratch;   // this device's copy of fftconv_static_scratch (device address)
-    int profiling;
-    hipEvent_t ev[2 * 8];   // start/stop pair per kernel of the last call
-    int nk;                 // kernels of the last call that carry events
-    const char *label[8];   // what each of them is (see fftconv_last_kernel_label)
-    char last_hip_error[256];
-};
 
 // Fourier bases of the 2-D transforms: the powers of two 8 ... 128 (Section 5 of the paper) and,
 // between them, sizes 2^a * {3, 5, 7, 9} from the search space of Section 3.4: one odd factor
@@ -295,12 +278,12 @@ static int cached_plan(fftconv_ctx *c, int pass, int S, int f, int fo, int h, in
     return FFTCONV_OK;
 }
 
-static int hip_fail(fftconv_ctx *c, hipError_t e) {
+int fc::hip_fail(fftconv_ctx *c, hipError_t e) {
     if (c) snprintf(c->last_hip_error, sizeof(c->last_hip_error), "HIP error: %s", hipGetErrorString(e));
     return FFTCONV_HIP_ERROR;
 }
 
-static int get_workspace(fftconv_ctx *c, size_t need, void **ws, size_t ws_bytes) {
+int fc::get_workspace(fftconv_ctx *c, size_t need, void **ws, size_t ws_bytes) {
     if (*ws) return ws_bytes < need ? FFTCONV_WORKSPACE_TOO_SMALL : FFTCONV_OK;
     hipError_t e;
     if (c->ws_bytes < need) {

@@ -1,0 +1,506 @@
+// Rows of a table by token, and the table's gradient.
+//
+//   fprop     y[n] = scale * table[token[n]]              (zero where n has no token)
+//   accGrad   gtable[v] = scale * sum over n with token[n] = v of gy[n]   (+ what was there)
+//
+// Both move bytes and compute next to nothing: fprop reads and writes each row once, accGrad reads
+// each row of gy once and writes each row of the table once.
+//
+// accGrad adds a token's rows in the order of n, whatever the launch: the tokens are sorted by a
+// stable radix sort (least significant digit first), the sorted list is cut into chunks of equal
+// length, and each chunk adds up its runs of equal tokens in fp32 registers.  A run that ends inside its
+// chunk is written straight to the table; what a chunk holds of a run that crosses its borders goes to the
+// workspace in fp32, and a second launch joins those parts, again in order.  So a token that half
+// of the text consists of costs what any other rows cost, and two calls give the same bits.
+#include "operands.hpp"
+
+namespace fc {
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4;
+
+// ---------------------------------------------------------------------------------- fprop
+template <class T>
+struct FpropArgs {
+    const T *table;
+    Tokens tok;
+    T *y;
+    long N;
+    int D, rows, cpr;     // rows per block, chunks of 8 elements per row
+    float scale;
+};
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void embedding_rows_kernel(FpropArgs<T> a) {
+    const long n0 = (long)blockIdx.x * a.rows;
+    const int rows = (int)(a.N - n0 < a.rows ? a.N - n0 : a.rows);
+    const unsigned total = (unsigned)rows * a.cpr;
+    for (unsigned c = threadIdx.x; c < total; c += kThreads) {
+        const unsigned r = c / (unsigned)a.cpr;
+        const int d = (int)(c - r * a.cpr) * 8, n = a.D - d;
+        const int t = a.tok(n0 + r);
+        float f[8] = {};
+        if (t >= 0) load8(a.table + (size_t)t * a.D + d, n, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] *= a.scale;
+        store8(a.y + (size_t)(n0 + r) * a.D + d, n, f);
+    }
+}
+
+// Planes: a tile of 64 positions by 64 features turns in LDS, so that rows are read along their features
+// and planes written along their positions.
+template <class T>
+struct PlaneArgs {
+    const T *table;
+    Tokens tok;
+    T *y;
+    int D, T_, tiles_t, tiles_d;
+    float scale;
+};
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void embedding_planes_kernel(PlaneArgs<T> a) {
+    __shared__ float tile[64][65];
+    const unsigned per = (unsigned)a.tiles_t * a.tiles_d;
+    const unsigned s = blockIdx.x / per, rest = blockIdx.x - s * per;
+    const int t0 = (int)(rest % a.tiles_t) * 64, d0 = (int)(rest / a.tiles_t) * 64;
+    for (int c = threadIdx.x; c < 64 * 8; c += kThreads) {
+        const int r = c >> 3, d = d0 + (c & 7) * 8;
+        float f[8] = {};
+        if (t0 + r < a.T_ && d < a.D) {
+            const int v = a.tok((long)s * a.T_ + t0 + r);
+            if (v >= 0) load8(a.table + (size_t)v * a.D + d, a.D - d, f);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) tile[(c & 7) * 8 + i][r] = f[i];
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if (t0 + lane < a.T_)
+        for (int i = w; i < 64 && d0 + i < a.D; i += kWaves)
+            a.y[((size_t)s * a.D + d0 + i) * a.T_ + t0 + lane] = (T)(tile[i][lane] * a.scale);
+}
+
+// The turn back: planes of gy to rows, for accGrad (rows without a token are not needed and skipped).
+template <class T>
+struct TurnArgs {
+    const T *gy;
+    Tokens tok;
+    T *rows;
+    int D, T_, tiles_t, tiles_d;
+};
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void planes_to_rows_kernel(TurnArgs<T> a) {
+    __shared__ float tile[64][65];
+    const unsigned per = (unsigned)a.tiles_t * a.tiles_d;
+    const unsigned s = blockIdx.x / per, rest = blockIdx.x - s * per;
+    const int t0 = (int)(rest % a.tiles_t) * 64, d0 = (int)(rest / a.tiles_t) * 64;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if (t0 + lane < a.T_)
+        for (int i = w; i < 64 && d0 + i < a.D; i += kWaves)
+            tile[i][lane] = to_float(a.gy[((size_t)s * a.D + d0 + i) * a.T_ + t0 + lane]);
+    __syncthreads();
+    for (int c = threadIdx.x; c < 64 * 8; c += kThreads) {
+        const int r = c >> 3, dd = (c & 7) * 8, n = a.D - d0 - dd;
+        if (t0 + r >= a.T_ || n <= 0) continue;
+        const long row = (long)s * a.T_ + t0 + r;
+        if (a.tok(row) < 0) continue;
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = i < n ? tile[dd + i][r] : 0.f;
+        store8(a.rows + (size_t)row * a.D + d0 + dd, n, f);
+    }
+}
+
+// ---------------------------------------------------------------------------------- sort
+constexpr int kDigitBits = 10, kDigits = 1 << kDigitBits;
+constexpr int kMaxBlocks = 512;
+
+struct SortPlan {
+    int passes, bits;     // digits, bits of one
+    int blocks;
+    long items;           // per block, a multiple of 256
+};
+SortPlan sort_plan(long N, int V) {
+    int bits = 1;
+    while (bits < 31 && (1L << bits) < V) ++bits;
+    SortPlan p;
+    p.passes = (bits + kDigitBits - 1) / kDigitBits;
+    p.bits = (bits + p.passes - 1) / p.passes;
+    p.items = ceil_to((N + kMaxBlocks - 1) / kMaxBlocks, kThreads);
+    if (p.items < 1024) p.items = 1024;
+    p.blocks = (int)((N + p.items - 1) / p.items);
+    return p;
+}
+
+struct SortArgs {
+    Tokens tok;               // the first pass reads these,
+    const int *key_in, *idx_in;   // the others these
+    int *key_out, *idx_out;
+    int *hist;                // [blocks][digits]
+    int *count;               // how many rows have a token
+    unsigned char *present;   // [V], first pass; null where nobody asks
+    long N, items;
+    int V, shift, bits, blocks;
+    int first;
+};
+
+__device__ __forceinline__ bool sort_item(const SortArgs &a, long at, long end, int &key, int &idx) {
+    key = -1; idx = 0;
+    if (at < end) {
+        if (a.first) { key = a.tok(at); idx = (int)at; }
+        else { key = a.key_in[at]; idx = a.idx_in[at]; }
+    }
+    return key >= 0;
+}
+
+__global__ __launch_bounds__(kThreads) void sort_count_kernel(SortArgs a) {
+    __shared__ int h[kDigits];
+    const int nd = 1 << a.bits;
+    for (int d = threadIdx.x; d < nd; d += kThreads) h[d] = 0;
+    if (a.first && a.present)
+        for (long v = (long)blockIdx.x * kThreads + threadIdx.x; v < a.V; v += (long)gridDim.x * kThreads) a.present[v] = 0;
+    __syncthreads();
+    const long n = a.first ? a.N : (long)*a.count;
+    const long begin = blockIdx.x * a.items, end = begin + a.items < n ? begin + a.items : n;
+    for (long at = begin + threadIdx.x; at < end; at += kThreads) {
+        int key, idx;
+        if (sort_item(a, at, end, key, idx)) atomicAdd(&h[(key >> a.shift) & (nd - 1)], 1);
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < nd; d += kThreads) a.hist[(size_t)blockIdx.x * nd + d] = h[d];
+}
+
+// Every block finds its own place for each digit from all blocks' counts, then places its items in
+// order: a wave takes a contiguous piece, 64 items at a time, and within those a lane's rank is
+// the number of lower lanes with the same digit.
+__global__ __launch_bounds__(kThreads) void sort_place_kernel(SortArgs a) {
+    __shared__ int base[kDigits];
+    __shared__ int mine[kWaves][kDigits];
+    __shared__ int part[kThreads];
+    const int nd = 1 << a.bits, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int per = (nd + kThreads - 1) / kThreads;     // neighbouring digits per thread
+    int sum = 0;
+    for (int i = 0; i < per; ++i) {
+        const int d = tid * per + i;
+        int all = 0, before = 0;
+        if (d < nd)
+            for (int b = 0; b < a.blocks; ++b) {
+                const int h = a.hist[(size_t)b * nd + d];
+                all += h;
+                before += b < (int)blockIdx.x ? h : 0;
+            }
+        if (d < nd) { base[d] = before + sum; sum += all; }
+    }
+    part[tid] = sum;
+    for (int d = tid; d < nd; d += kThreads)
+#pragma unroll
+        for (int q = 0; q < kWaves; ++q) mine[q][d] = 0;
+    __syncthreads();
+    for (int step = 1; step < kThreads; step <<= 1) {
+        const int v = tid >= step ? part[tid - step] : 0;
+        __syncthreads();
+        part[tid] += v;
+        __syncthreads();
+    }
+    const int offset = part[tid] - sum;
+    for (int i = 0; i < per; ++i)
+        if (tid * per + i < nd) base[tid * per + i] += offset;
+    if (a.first && blockIdx.x == 0 && tid == kThreads - 1) *a.count = part[tid];
+
+    const long n = a.first ? a.N : (long)*a.count;
+    const long wave_items = a.items / kWaves;
+    const long begin = blockIdx.x * a.items + w * wave_items;
+    const long stop = begin + wave_items < n ? begin + wave_items : n;
+    // how many of each digit the earlier waves of this block hold
+    for (long at = begin; at < stop; at += 64) {
+        int key, idx;
+        if (sort_item(a, at + lane, stop, key, idx)) atomicAdd(&mine[w][(key >> a.shift) & (nd - 1)], 1);
+    }
+    __syncthreads();
+    for (int d = tid; d < nd; d += kThreads) {
+        int at = base[d];
+#pragma unroll
+        for (int q = 0; q < kWaves; ++q) { const int c = mine[q][d]; mine[q][d] = at; at += c; }
+    }
+    __syncthreads();
+    for (long at = begin; at < stop; at += 64) {
+        int key, idx;
+        const bool has = sort_item(a, at + lane, stop, key, idx);
+        const int digit = (key >> a.shift) & (nd - 1);
+        unsigned long long same = __ballot(has);
+        for (int b = 0; b < a.bits; ++b) {
+            const unsigned long long set = __ballot((digit >> b) & 1);
+            same &= (digit >> b) & 1 ? set : ~set;
+        }
+        const int rank = __popcll(same & ((1ull << lane) - 1));
+        int place = 0;
+        if (has) place = mine[w][digit] + rank;
+        __builtin_amdgcn_wave_barrier();
+        if (has && rank == 0) mine[w][digit] += __popcll(same);
+        __builtin_amdgcn_wave_barrier();
+        if (has) {
+            a.key_out[place] = key;
+            a.idx_out[place] = idx;
+            if (a.first && a.present) a.present[key] = 1;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------- sums
+template <class T>
+struct SumArgs {
+    const T *gy;
+    const int *key, *idx;     // sorted
+    const int *count;
+    const unsigned char *present;
+    T *gtable;
+    float *head, *tail;       // [chunks][D]: a chunk's part of the run that began before it / that goes on after it
+    long chunks;
+    int D, V, C;              // C: sorted positions per chunk
+    int lanes;                // threads of one row: a power of two, 8 elements each
+    int slices;               // pieces of 8 * lanes elements in a row
+    long sum_blocks;          // the blocks behind these write zeros to the rows no token names
+    int zero_rows;            // rows per such block
+    float scale;
+    int accumulate;
+};
+
+template <class T>
+__device__ __forceinline__ void finish_row(const SumArgs<T> &a, int key, int d, int n, const float (&acc)[8]) {
+    T *to = a.gtable + (size_t)key * a.D + d;
+    float f[8];
+    if (a.accumulate) {
+        load8(to, n, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] += acc[i] * a.scale;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = acc[i] * a.scale;
+    }
+    store8(to, n, f);
+}
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void embedding_sum_kernel(SumArgs<T> a) {
+    const int tid = threadIdx.x;
+    if ((long)blockIdx.x >= a.sum_blocks) {
+        const long v0 = ((long)blockIdx.x - a.sum_blocks) * a.zero_rows;
+        const int cpr = (a.D + 7) / 8;
+        const float zero[8] = {};
+        for (int c = tid; c < a.zero_rows * cpr; c += kThreads) {
+            const int r = c / cpr, d = (c - r * cpr) * 8;
+            if (v0 + r < a.V && !a.present[v0 + r]) store8(a.gtable + (size_t)(v0 + r) * a.D + d, a.D - d, zero);
+        }
+        return;
+    }
+    const long groups = kThreads / a.lanes;
+    const long unit = blockIdx.x * groups + tid / a.lanes;
+    const long chunk = unit / a.slices;
+    const int d = ((int)(unit - chunk * a.slices) * a.lanes + tid % a.lanes) * 8, n = a.D - d;
+    const long cnt = *a.count, begin = chunk * a.C;
+    if (begin >= cnt || n <= 0) return;
+    const long end = begin + a.C < cnt ? begin + a.C : cnt;
+    const int before = begin > 0 ? a.key[begin - 1] : -1, after = end < cnt ? a.key[end] : -1;
+    int key = a.key[begin];
+    float acc[8] = {};
+    constexpr int U = 4;
+    for (long p = begin; p < end; p += U) {
+        float row[U][8];
+        int k[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long at = p + u < end ? p + u : end - 1;
+            k[u] = a.key[at];
+            load8(a.gy + (size_t)a.idx[at] * a.D + d, n, row[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (p + u >= end) break;
+            if (k[u] != key) {
+                if (key == before) store8(a.head + (size_t)chunk * a.D + d, n, acc);
+                else finish_row(a, key, d, n, acc);
+                key = k[u];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] += row[u][i];
+        }
+    }
+    if (key == before) store8(a.head + (size_t)chunk * a.D + d, n, acc);
+    else if (key == after) store8(a.tail + (size_t)chunk * a.D + d, n, acc);
+    else finish_row(a, key, d, n, acc);
+}
+
+// One block for each chunk in which a run begins that the chunk does not end.
+template <class T>
+__global__ __launch_bounds__(kThreads) void embedding_join_kernel(SumArgs<T> a) {
+    __shared__ float sums[kThreads][9];
+    const long chunk = blockIdx.x, cnt = *a.count, begin = chunk * a.C, end = begin + a.C;
+    if (end >= cnt) return;                              // (nothing after it)
+    const int key = a.key[end - 1];
+    if (a.key[end] != key || (begin > 0 && a.key[begin - 1] == key)) return;
+    long lo = end, hi = cnt;                             // the run's end: the first position behind it
+    while (lo < hi) {
+        const long mid = (lo + hi) / 2;
+        if (a.key[mid] == key) lo = mid + 1; else hi = mid;
+    }
+    const long last = (lo - 1) / a.C;                    // the chunk it ends in
+    const int groups = kThreads / a.lanes, g = threadIdx.x / a.lanes, l = threadIdx.x % a.lanes;
+    // group g adds the parts of a stretch of neighbouring chunks, then the stretches are added in order
+    const long parts = last - chunk + 1, each = (parts + groups - 1) / groups;
+    const long from = chunk + g * each, to = from + each <= last + 1 ? from + each : last + 1;
+    for (int s = 0; s < a.slices; ++s) {
+        const int d = (s * a.lanes + l) * 8, n = a.D - d;
+        float acc[8] = {};
+        if (n > 0)
+            for (long c = from; c < to; ++c) {
+                float f[8];
+                load8((c == chunk ? a.tail : a.head) + (size_t)c * a.D + d, n, f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] += f[i];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[threadIdx.x][i] = acc[i];
+        __syncthreads();
+        if (g == 0 && n > 0) {
+            for (int q = 1; q < groups; ++q)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] += sums[q * a.lanes + l][i];
+            finish_row(a, key, d, n, acc);
+        }
+    }
+}
+
+struct GradPlan {
+    SortPlan sort;
+    int lanes, slices, C;
+    long chunks;
+    size_t rows, key[2], idx[2], hist, count, present, head, tail, total;
+};
+GradPlan grad_plan(int dtype, long N, int D, int V, int T) {
+    GradPlan p;
+    p.sort = sort_plan(N, V);
+    const int cpr = (D + 7) / 8;
+    p.lanes = 1;
+    while (p.lanes < cpr && p.lanes < kThreads) p.lanes *= 2;
+    p.slices = (cpr + p.lanes - 1) / p.lanes;
+    // chunks short enough for 64k threads, long enough that the parts they leave are few
+    const long c = N * (long)cpr / 65536;
+    p.C = (int)(c < 8 ? 8 : c > 64 ? 64 : c);
+    p.chunks = (N + p.C - 1) / p.C;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t o = at; at = up(at + bytes, 256); return o; };
+    p.rows = take(T ? (size_t)N * D * type_bytes(dtype) : 0);
+    for (int i = 0; i < 2; ++i) { p.key[i] = take((size_t)N * 4); p.idx[i] = take((size_t)N * 4); }
+    p.hist = take((size_t)p.sort.blocks * (4u << p.sort.bits));
+    p.count = take(4);
+    p.present = take(V);
+    p.head = take((size_t)p.chunks * D * 4);
+    p.tail = take((size_t)p.chunks * D * 4);
+    p.total = at;
+    return p;
+}
+
+template <class T>
+hipError_t fprop(const void *table, Tokens tok, void *y, long N, int D, int Tn, float scale, hipStream_t s) {
+    if (Tn) {
+        PlaneArgs<T> a{static_cast<const T *>(table), tok, static_cast<T *>(y), D, Tn, (Tn + 63) / 64, (D + 63) / 64, scale};
+        const long blocks = N / Tn * a.tiles_t * a.tiles_d;
+        if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
+        hipLaunchKernelGGL(embedding_planes_kernel<T>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+        return hipGetLastError();
+    }
+    FpropArgs<T> a{static_cast<const T *>(table), tok, static_cast<T *>(y), N, D, 1, (D + 7) / 8, scale};
+    // four chunks a thread, but no fewer than a thousand blocks for it
+    const long most = 1024 / a.cpr, share = (N + 1023) / 1024;
+    a.rows = (int)(most < 1 ? 1 : most < share ? most : share);
+    hipLaunchKernelGGL(embedding_rows_kernel<T>, dim3((unsigned)((N + a.rows - 1) / a.rows)), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, int D, int Tn, float scale, bool accumulate,
+                   char *ws, hipStream_t s) {
+    const int V = tok.V;
+    const GradPlan p = grad_plan(dtype, N, D, V, Tn);
+    const T *rows = static_cast<const T *>(gy);
+    if (Tn) {
+        TurnArgs<T> t{rows, tok, reinterpret_cast<T *>(ws + p.rows), D, Tn, (Tn + 63) / 64, (D + 63) / 64};
+        const long blocks = N / Tn * t.tiles_t * t.tiles_d;
+        if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
+        hipLaunchKernelGGL(planes_to_rows_kernel<T>, dim3((unsigned)blocks), dim3(kThreads), 0, s, t);
+        rows = t.rows;
+    }
+    SortArgs so{};
+    so.tok = tok;
+    so.hist = reinterpret_cast<int *>(ws + p.hist);
+    so.count = reinterpret_cast<int *>(ws + p.count);
+    so.present = accumulate ? nullptr : reinterpret_cast<unsigned char *>(ws + p.present);
+    so.N = N; so.items = p.sort.items; so.V = V; so.bits = p.sort.bits; so.blocks = p.sort.blocks;
+    for (int i = 0; i < p.sort.passes; ++i) {
+        so.first = i == 0;
+        so.shift = i * p.sort.bits;
+        so.key_in = reinterpret_cast<int *>(ws + p.key[(i + 1) & 1]);
+        so.idx_in = reinterpret_cast<int *>(ws + p.idx[(i + 1) & 1]);
+        so.key_out = reinterpret_cast<int *>(ws + p.key[i & 1]);
+        so.idx_out = reinterpret_cast<int *>(ws + p.idx[i & 1]);
+        hipLaunchKernelGGL(sort_count_kernel, dim3(so.blocks), dim3(kThreads), 0, s, so);
+        hipLaunchKernelGGL(sort_place_kernel, dim3(so.blocks), dim3(kThreads), 0, s, so);
+    }
+    SumArgs<T> a{};
+    a.gy = rows;
+    a.key = so.key_out; a.idx = so.idx_out; a.count = so.count; a.present = so.present;
+    a.gtable = static_cast<T *>(gtable);
+    a.head = reinterpret_cast<float *>(ws + p.head);
+    a.tail = reinterpret_cast<float *>(ws + p.tail);
+    a.chunks = p.chunks; a.D = D; a.V = V; a.C = p.C; a.lanes = p.lanes; a.slices = p.slices;
+    a.scale = scale; a.accumulate = accumulate;
+    const long groups = kThreads / p.lanes;
+    a.sum_blocks = (p.chunks * p.slices + groups - 1) / groups;
+    const int cpr = (D + 7) / 8;
+    a.zero_rows = 1024 / cpr < 1 ? 1 : 1024 / cpr > 64 ? 64 : 1024 / cpr;
+    const long zero_blocks = accumulate ? 0 : ((long)V + a.zero_rows - 1) / a.zero_rows;
+    if (a.sum_blocks + zero_blocks > 0x7fffffffL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(embedding_sum_kernel<T>, dim3((unsigned)(a.sum_blocks + zero_blocks)), dim3(kThreads), 0, s, a);
+    if (p.chunks > 1)
+        hipLaunchKernelGGL(embedding_join_kernel<T>, dim3((unsigned)p.chunks), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void zero_kernel(T *p, size_t n) {
+    for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (size_t)gridDim.x * kThreads) p[i] = (T)0.f;
+}
+
+}  // namespace
+
+size_t embedding_accgrad_bytes(int dtype, long N, int D, int V, int T) { return N ? grad_plan(dtype, N, D, V, T).total : 0; }
+
+hipError_t launch_embedding_fprop(int dtype, const void *table, Tokens tok, void *y, long N, int D, int T, float scale, hipStream_t s) {
+    if (N == 0) return hipSuccess;
+    if (dtype == kF32) return fprop<float>(table, tok, y, N, D, T, scale, s);
+    if (dtype == kBF16) return fprop<__bf16>(table, tok, y, N, D, T, scale, s);
+    return fprop<_Float16>(table, tok, y, N, D, T, scale, s);
+}
+
+hipError_t launch_embedding_accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, int D, int T, float scale,
+                                    bool accumulate, void *ws, hipStream_t s) {
+    if (N == 0) {
+        if (accumulate) return hipSuccess;
+        const size_t n = (size_t)tok.V * D;
+        const unsigned blocks = (unsigned)(n / kThreads + 1 < 4096 ? n / kThreads + 1 : 4096);
+        if (dtype == kF32) hipLaunchKernelGGL(zero_kernel<float>, dim3(blocks), dim3(kThreads), 0, s, static_cast<float *>(gtable), n);
+        else hipLaunchKernelGGL(zero_kernel<__bf16>, dim3(blocks), dim3(kThreads), 0, s, static_cast<__bf16 *>(gtable), n);
+        return hipGetLastError();
+    }
+    char *w = static_cast<char *>(ws);
+    if (dtype == kF32) return accgrad<float>(dtype, gy, tok, gtable, N, D, T, scale, accumulate, w, s);
+    if (dtype == kBF16) return accgrad<__bf16>(dtype, gy, tok, gtable, N, D, T, scale, accumulate, w, s);
+    return accgrad<_Float16>(dtype, gy, tok, gtable, N, D, T, scale, accumulate, w, s);
+}
+
+}  // namespace fc

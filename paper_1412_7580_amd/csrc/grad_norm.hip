@@ -1,0 +1,185 @@
+// The 2-norm of many tensors taken together, and their scaling to a largest norm:
+//
+//   norm = sqrt(sum over all elements of g^2),   out = g * min(1, max_norm / norm)
+//
+// The norm reads every element once; clipping reads it once more and writes it once (the coefficient
+// is known only when all have been read).  Squares and sums are held in 64 bits: no gradient's square
+// leaves that range, and a thousand million terms lose nothing that the fp32 result could show.
+// The tensors are cut into pieces of equal length; a block adds up one piece and leaves its sum in the
+// workspace, and whoever needs the norm adds all of those in the same order: the result does not
+// depend on the order in which blocks run.  The list of tensors travels in the kernel's arguments, so
+// nothing is copied to the device and a captured call holds its list itself.
+//
+// A norm that is zero, infinite or not a number leaves the tensors as they are: the caller sees it in `norm`.
+#include "operands.hpp"
+
+namespace fc {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPerLaunch = 128;          // tensors in one launch's arguments (29 bytes each, of 4096)
+constexpr long kPieces = 4096, kLeast = 8192;
+
+struct NormArgs {
+    const void *in[kPerLaunch];
+    void *out[kPerLaunch];
+    long size[kPerLaunch];
+    int first[kPerLaunch + 1];           // number of the tensor's first piece within this launch
+    unsigned char dtype[kPerLaunch];
+    int count, base;                     // tensors, pieces of earlier launches
+    long piece;                          // elements, a multiple of 8
+    double *sums;
+    float *norm;
+    int pieces;                          // of all launches
+    float max_norm;
+};
+
+__device__ __forceinline__ int tensor_of(const NormArgs &a, int p) {
+    int lo = 0, hi = a.count;            // the last tensor whose first piece is not behind p
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (a.first[mid] <= p) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ double block_sum(double v, double *lds) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+
+template <class T>
+__device__ __forceinline__ double squares(const T *p, long n) {
+    double s = 0;
+    constexpr int U = 4;
+    long i = (long)threadIdx.x * 8;
+    for (; i + (U - 1) * kThreads * 8L + 8 <= n; i += U * kThreads * 8L) {
+        float f[U][8];
+#pragma unroll
+        for (int u = 0; u < U; ++u) load8(p + i + u * kThreads * 8L, 8, f[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s = fma((double)f[u][j], (double)f[u][j], s);
+    }
+    for (; i < n; i += kThreads * 8L) {
+        float f[8];
+        load8(p + i, (int)(n - i < 8 ? n - i : 8), f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s = fma((double)f[j], (double)f[j], s);
+    }
+    return s;
+}
+
+__global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a) {
+    __shared__ double lds[4];
+    const int p = blockIdx.x, t = tensor_of(a, p);
+    const long from = (long)(p - a.first[t]) * a.piece;
+    const long n = a.size[t] - from < a.piece ? a.size[t] - from : a.piece;
+    double s;
+    if (a.dtype[t] == kF32) s = squares(static_cast<const float *>(a.in[t]) + from, n);
+    else if (a.dtype[t] == kBF16) s = squares(static_cast<const __bf16 *>(a.in[t]) + from, n);
+    else s = squares(static_cast<const _Float16 *>(a.in[t]) + from, n);
+    s = block_sum(s, lds);
+    if (threadIdx.x == 0) a.sums[a.base + p] = s;
+}
+
+__device__ __forceinline__ double total(const double *sums, int pieces, double *lds) {
+    double s = 0;
+    for (int i = threadIdx.x; i < pieces; i += kThreads) s += sums[i];
+    return block_sum(s, lds);
+}
+
+__global__ __launch_bounds__(kThreads) void norm_end_kernel(const double *sums, int pieces, float *norm) {
+    __shared__ double lds[4];
+    const double s = total(sums, pieces, lds);
+    if (threadIdx.x == 0) *norm = (float)sqrt(s);
+}
+
+template <class T>
+__device__ __forceinline__ void scaled(const T *in, T *out, long n, float c) {
+    for (long i = (long)threadIdx.x * 8; i < n; i += kThreads * 8L) {
+        const int m = (int)(n - i < 8 ? n - i : 8);
+        float f[8];
+        load8(in + i, m, f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] *= c;
+        store8(out + i, m, f);
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void clip_kernel(NormArgs a) {
+    __shared__ double lds[4];
+    const double norm = sqrt(total(a.sums, a.pieces, lds));
+    if (a.base == 0 && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
+    const bool clip = norm > (double)a.max_norm && norm < 1.7e308;
+    const float c = clip ? (float)((double)a.max_norm / norm) : 1.f;
+    const int p = blockIdx.x, t = tensor_of(a, p);
+    if (!clip && a.in[t] == a.out[t]) return;
+    const long from = (long)(p - a.first[t]) * a.piece;
+    const long n = a.size[t] - from < a.piece ? a.size[t] - from : a.piece;
+    if (a.dtype[t] == kF32) scaled(static_cast<const float *>(a.in[t]) + from, static_cast<float *>(a.out[t]) + from, n, c);
+    else if (a.dtype[t] == kBF16) scaled(static_cast<const __bf16 *>(a.in[t]) + from, static_cast<__bf16 *>(a.out[t]) + from, n, c);
+    else scaled(static_cast<const _Float16 *>(a.in[t]) + from, static_cast<_Float16 *>(a.out[t]) + from, n, c);
+}
+
+long piece_length(int count, const long *sizes) {
+    long total = 0;
+    for (int i = 0; i < count; ++i) total += sizes[i];
+    const long even = ceil_to((total + kPieces - 1) / kPieces, 2048);
+    return even < kLeast ? kLeast : even;
+}
+long pieces_of(int count, const long *sizes, long piece) {
+    long n = 0;
+    for (int i = 0; i < count; ++i) n += (sizes[i] + piece - 1) / piece;
+    return n;
+}
+
+}  // namespace
+
+size_t grad_norm_bytes(int count, const long *sizes) {
+    return up((size_t)pieces_of(count, sizes, piece_length(count, sizes)) * sizeof(double), 256);
+}
+
+hipError_t launch_grad_norm(int count, const void *const *grads, const long *sizes, const int *dtypes, void *const *out,
+                            float max_norm, float *norm, void *ws, hipStream_t s) {
+    NormArgs a;
+    a.piece = piece_length(count, sizes);
+    const long pieces = pieces_of(count, sizes, a.piece);
+    if (pieces > 0x7fffffffL) return hipErrorInvalidValue;
+    a.sums = static_cast<double *>(ws);
+    a.norm = norm;
+    a.max_norm = max_norm;
+    a.pieces = (int)pieces;
+    for (int clip = 0; clip < (out ? 2 : 1); ++clip) {
+        int base = 0;
+        for (int i = 0; i < count;) {
+            a.count = 0;
+            a.base = base;
+            int n = 0;
+            for (; i < count && a.count < kPerLaunch; ++i) {
+                if (sizes[i] == 0) continue;
+                const int k = a.count++;
+                a.in[k] = grads[i];
+                a.out[k] = out ? out[i] : nullptr;
+                a.size[k] = sizes[i];
+                a.dtype[k] = (unsigned char)dtypes[i];
+                a.first[k] = n;
+                n += (int)((sizes[i] + a.piece - 1) / a.piece);
+            }
+            a.first[a.count] = n;
+            if (!a.count) break;
+            if (clip) hipLaunchKernelGGL(clip_kernel, dim3(n), dim3(kThreads), 0, s, a);
+            else hipLaunchKernelGGL(norm_kernel, dim3(n), dim3(kThreads), 0, s, a);
+            base += n;
+        }
+    }
+    if (!out || !pieces)
+        hipLaunchKernelGGL(norm_end_kernel, dim3(1), dim3(kThreads), 0, s, static_cast<const double *>(ws), (int)pieces, norm);
+    return hipGetLastError();
+}
+
+}  // namespace fc
