@@ -20,7 +20,7 @@
 // A tile is staged with direct global-to-LDS loads of 16 bytes a lane, one K step ahead, in two
 // buffers.  LDS is written in lane order, so the swizzle that spreads a column of 16-byte pieces over
 // the banks is applied to the addresses that are read: piece c of row r holds what belongs to
-// c ^ (r & 7) (K inside), or c ^ 2 (r & 3) (K outside).
+// c ^ (r & 7) (K inside), or c ^ (2 (r & 3) | (r & 8)) (K outside).
 #pragma once
 #include "operands.hpp"
 #include "kernels.hpp"
@@ -70,15 +70,28 @@ struct GemmArgs {
     int add;                 // add to what `partial` or `out` holds
     void *out;
     long out_ld;
-    const float *alpha_scale;    // factor on the device
-    float alpha;
+    const float *alpha_scale;    // factor of `out`, on the device
 };
 
 __device__ __forceinline__ void lds_load16(const char *from, unsigned lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
 }
+__device__ __forceinline__ const char *uniform(const char *p) {
+    const unsigned long u = (unsigned long)p;
+    const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)u), hi = __builtin_amdgcn_readfirstlane((unsigned)(u >> 32));
+    return (const char *)((unsigned long)hi << 32 | lo);
+}
+__device__ __forceinline__ void lds_load16(const char *base, unsigned off, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void lds_load4(const void *base, unsigned off, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void lds_written_and_met() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// Every wave's staging loads but its last N have landed, its LDS reads are done, and all waves are here.
+template <int N>
 __device__ __forceinline__ void landed_and_met() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
 template <class T> struct Mfma;
@@ -96,43 +109,44 @@ template <int R, int W, bool KIN>
 struct Tile {
     static constexpr int kLoads = R * 128 / 1024 / W;        // 1 KB a wave
     static constexpr int kPieces = R / 8;                    // 16-byte pieces in a row of 64 (K outside)
-    const char *at[kLoads];                                  // K inside: the lane's place in step 0
-    int col[kLoads];                                         // K inside: its column there; K outside: its k
-    long across;                                             // K outside: its byte column
+    const char *base;                                        // first row of the result's side, k = 0
+    unsigned off[kLoads];                                    // the lane's bytes from there
 
+    static __device__ __forceinline__ int swizzle(int k) { return 2 * (k & 3) | (k & 8); }
+    // Row (K inside) or k (K outside) and column of the lane's piece i.
+    static __device__ __forceinline__ void place(int i, int w, int lane, int &r, int &c) {
+        const int piece = (i * W + w) * 64 + lane;           // of 16 bytes, in LDS order
+        if (KIN) { r = piece >> 3; c = ((piece & 7) ^ (r & 7)) * 8; }
+        else { r = piece / kPieces; c = ((piece % kPieces) ^ swizzle(r)) * 8; }
+    }
     // first: the tile's first row of the result's side.  KIN: rows of memory, else columns.
     __device__ __forceinline__ void begin(const GemmSide &g, long first, int w, int lane) {
+        base = static_cast<const char *>(g.p) + (KIN ? first * g.ld : first) * 2;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int piece = (i * W + w) * 64 + lane;       // of 16 bytes, in LDS order
-            if (KIN) {
-                const int r = piece >> 3, c = (piece & 7) ^ (r & 7);
-                long row = first + r;
-                if (row >= g.rows) row = g.rows - 1;
-                col[i] = c * 8;
-                at[i] = static_cast<const char *>(g.p) + (row * g.ld + c * 8) * 2;
-            } else {
-                const int k = piece / kPieces, c = (piece % kPieces) ^ (2 * (k & 3));
-                col[i] = k;
-                long x = first + c * 8;
-                if (x >= g.cols) x = 0;
-                at[i] = static_cast<const char *>(g.p) + x * 2;
-            }
+            int r, c;
+            place(i, w, lane, r, c);
+            if (KIN) { if (first + r >= g.rows) r = (int)(g.rows - 1 - first); }
+            else if (first + c >= g.cols) c = 0;
+            off[i] = (unsigned)(((long)r * g.ld + c) * 2);
         }
     }
-    __device__ __forceinline__ void load(const GemmSide &g, const void *zeros, int k0, int term, unsigned lds, int w) const {
+    __device__ __forceinline__ void load(const GemmSide &g, const void *zeros, int k0, int term, unsigned lds, int w, int lane) const {
+        const char *from = uniform(base + (KIN ? k0 : k0 * g.ld) * 2 + term * g.term * 2);
+        if (k0 + kStep <= (KIN ? (long)g.cols : g.rows)) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const char *from;
-            if (KIN) {
-                from = at[i] + ((long)k0 + term * g.term) * 2;
-                if (col[i] + k0 >= g.cols) from = static_cast<const char *>(zeros);
-            } else {
-                long row = (long)k0 + col[i];
-                if (row >= g.rows) row = g.rows - 1;
-                from = at[i] + (row * g.ld + term * g.term) * 2;
+            for (int i = 0; i < kLoads; ++i) lds_load16(from, off[i], lds + (i * W + w) * 1024);
+        } else {
+            asm volatile("" : "+v"(lane));                   // (what follows from it is formed here, not kept in registers)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                int r, c;
+                place(i, w, lane, r, c);
+                const char *at = from + off[i];
+                if (KIN) { if (k0 + c >= g.cols) at = static_cast<const char *>(zeros); }
+                else if (k0 + r >= g.rows) at += (g.rows - 1 - k0 - r) * g.ld * 2;
+                lds_load16(at, lds + (i * W + w) * 1024);
             }
-            lds_load16(from, lds + (i * W + w) * 1024);
         }
     }
     // The 16 rows from r0 on, 32 k from 32 ks on, as the matrix cores take them: lane l holds row
@@ -148,7 +162,7 @@ struct Tile {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int k = ks * 32 + (lane >> 4) * 8 + h * 4 + (i >> 2);
-                const int c = ((r0 >> 3) + ((i & 3) >> 1)) ^ (2 * (k & 3));
+                const int c = ((r0 >> 3) + ((i & 3) >> 1)) ^ swizzle(k);
                 const char *p = lds + k * (R * 2) + c * 16 + (i & 1) * 8;
                 u.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v *)(p));
             }
@@ -157,52 +171,57 @@ struct Tile {
     }
 };
 
-// Tile of FM*WM*16 rows (m) by FN*WN*16 columns (n); a wave has FM*16 by FN*16 of it.
+constexpr int xent_lds_bytes(int bm, int bn, int wn) { return 2 * (bm + bn) * 128 + 2 * 3 * bm * 4 + wn * bm * 8; }
+
+// Tiles of FM*WM*16 rows (m) by FN*WN*16 columns (n); a wave has FM*16 by FN*16 of one.  A block takes
+// tiles until there are none left: the next one's first two steps are on their way while the
+// last one's end is computed.
 template <class T, int FM, int FN, int WM, int WN, int END, bool SPLIT>
 __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
     constexpr int BM = FM * WM * 16, BN = FN * WN * 16, W = WM * WN;
     constexpr bool PIN = END != kClasses, QIN = END == kStats || END == kGrad;
+    constexpr int kRowValues = END == kStats ? 1 : END == kGrad ? 3 : 0;      // target, lse, coef
     typedef typename Mfma<T>::frag F;
+    typedef Tile<BM, W, PIN> TP;
+    typedef Tile<BN, W, QIN> TQ;
     extern __shared__ __align__(1024) char lds[];
     constexpr int kBytes = (BM + BN) * 128;
+    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char *)lds;
+    char *const row_values = lds + 2 * kBytes;                                // [2][3][BM]
+    float2 *const both = reinterpret_cast<float2 *>(lds + 2 * kBytes + 2 * 3 * BM * 4);   // [WN][BM]
 
     const int count = *a.count;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = w / WN, wn = w % WN;
+    const int live_m = (count + BM - 1) / BM;
+    const int tiles_m = END == kClasses || a.tiles_m < live_m ? a.tiles_m : live_m;
+    const int total = tiles_m * a.tiles_n, units = total * a.splits;
+    const int K = END == kClasses ? count : a.K, steps = (K + kStep - 1) / kStep;
+    constexpr int kTerms = SPLIT ? 6 : 1;
 
+    TP tp;
+    TQ tq;
+    long m0, n0;
+    int tn, split, first, last;
     // Neighbouring blocks go to different XCDs: each XCD takes a contiguous eighth of the tiles, walked
     // in columns of four tiles so that what its L2 holds is used several times.
-    const int total = a.tiles_m * a.tiles_n;
-    const int split = blockIdx.x / total;
-    int id = blockIdx.x - split * total;
-    {
+    auto place = [&](int u) {
+        split = u / total;
+        int id = u - split * total;
         const int per = total / 8, more = total % 8, x = id % 8;
         id = x * per + (x < more ? x : more) + id / 8;
-    }
-    constexpr int GN = 4;
-    const int group = id / (GN * a.tiles_m), in = id - group * GN * a.tiles_m;
-    const int gn = a.tiles_n - group * GN < GN ? a.tiles_n - group * GN : GN;
-    const int tm = in / gn, tn = group * GN + in % gn;
-    const long m0 = (long)tm * BM, n0 = (long)tn * BN;
-    if (END != kClasses && m0 >= count) return;
-
-    const int K = END == kClasses ? count : a.K;
-    int steps = (K + kStep - 1) / kStep, begin = 0;
-    if (a.splits > 1) {
-        const int each = (steps + a.splits - 1) / a.splits;
-        begin = split * each;
-        steps = steps < begin + each ? steps : begin + each;
-    }
-
-    Tile<BM, W, PIN> tp;
-    Tile<BN, W, QIN> tq;
-    tp.begin(a.P, m0, w, lane);
-    tq.begin(a.Q, n0, w, lane);
-    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char *)lds;
-
-    constexpr int kTerms = SPLIT ? 6 : 1;
-    floatx4 acc[FM][FN] = {};
-    const int first = begin * kTerms, last = steps * kTerms;
+        constexpr int GN = 4;
+        const int group = id / (GN * tiles_m), in = id - group * GN * tiles_m;
+        const int gn = a.tiles_n - group * GN < GN ? a.tiles_n - group * GN : GN;
+        tn = group * GN + in % gn;
+        m0 = (long)(in / gn) * BM;
+        n0 = (long)tn * BN;
+        const int each = (steps + a.splits - 1) / a.splits, begin = split * each;
+        first = begin * kTerms;
+        last = (steps < begin + each ? steps : begin + each) * kTerms;
+        tp.begin(a.P, m0, w, lane);
+        tq.begin(a.Q, n0, w, lane);
+    };
     auto stage = [&](int s) {
         const int k0 = (SPLIT ? s / 6 : s) * kStep;
         int tp_ = 0, tq_ = 0;                                // terms: l h, h l, m m, m h, h m, h h
@@ -212,138 +231,223 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
             tq_ = t == 1 ? 2 : t == 2 || t == 4 ? 1 : 0;
         }
         const unsigned to = lds0 + (s & 1) * kBytes;
-        tp.load(a.P, a.zeros, k0, tp_, to, w);
-        tq.load(a.Q, a.zeros, k0, tq_, to + BM * 128, w);
+        tp.load(a.P, a.zeros, k0, tp_, to, w, lane);
+        tq.load(a.Q, a.zeros, k0, tq_, to + BM * 128, w, lane);
     };
-    if (first < last) stage(first);
-    for (int s = first; s < last; ++s) {
-        landed_and_met();
-        if (s + 1 < last) stage(s + 1);
+    // The first two steps, and before them the values that the tile's rows bring along.
+    auto stage_first = [&](int parity) {
+        if constexpr (kRowValues > 0) {
+            for (int i = w; i < kRowValues * (BM / 64); i += W) {
+                const int which = i / (BM / 64), at = i % (BM / 64);
+                const void *from = which == 0 ? (const void *)(a.target + m0) : which == 1 ? (const void *)(a.lse + m0) : (const void *)(a.coef + m0);
+                lds_load4(uniform(static_cast<const char *>(from)), (at * 64 + lane) * 4, lds0 + 2 * kBytes + ((parity * 3 + which) * BM + at * 64) * 4);
+            }
+        }
+        if (first < last) stage(first);
+        if (first + 1 < last) stage(first + 1);
+    };
+    struct Frags { F p[FM], q[FN]; };
+    floatx4 acc[FM][FN];
+    auto read = [&](Frags &f, int s, int ks) {
         const char *p = lds + (s & 1) * kBytes, *q = p + BM * 128;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            F fp[FM], fq[FN];
+        for (int j = 0; j < FN; ++j) f.q[j] = TQ::template frag<F>(q, (wn * FN + j) * 16, ks, lane);
 #pragma unroll
-            for (int j = 0; j < FN; ++j) fq[j] = Tile<BN, W, QIN>::template frag<F>(q, (wn * FN + j) * 16, ks, lane);
+        for (int i = 0; i < FM; ++i) f.p[i] = TP::template frag<F>(p, (wm * FM + i) * 16, ks, lane);
+    };
+    auto multiply = [&](const Frags &f) {
 #pragma unroll
-            for (int i = 0; i < FM; ++i) fp[i] = Tile<BM, W, PIN>::template frag<F>(p, (wm * FM + i) * 16, ks, lane);
+        for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
+            for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<T>::mul(f.q[j], f.p[i], acc[i][j]);
+    };
+    // Reads of one half step between the matrix instructions of the other.
+    auto interleave = [&]() {
+        constexpr int reads = FM * (PIN ? 1 : 2) + FN * (QIN ? 1 : 2), each = FM * FN / reads;
 #pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<T>::mul(fq[j], fp[i], acc[i][j]);
+        for (int r = 0; r < reads; ++r) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, each, 0);
         }
-    }
+        __builtin_amdgcn_sched_group_barrier(0x008, FM * FN - reads * each, 0);
+    };
 
-    // A lane holds, of each 16x16 tile, row lane & 15 and the four columns from 4 (lane >> 4) on.
-    const int row = lane & 15, quad = (lane >> 4) * 4;
-    if constexpr (END == kStats) {
-        landed_and_met();                                     // (the tiles in LDS are done with)
-        float2 *both = reinterpret_cast<float2 *>(lds);      // [WN][BM]
+    int u = blockIdx.x, parity = 0;
+    if (u >= units) return;
+    place(u);
+    stage_first(0);
+    for (;;) {
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const long m = m0 + (wm * FM + i) * 16 + row;
-            const int t = m < count ? a.target[m] : -1;
-            float top = -INFINITY;
+        for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int j = 0; j < FN; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const long n = n0 + (wn * FN + j) * 16 + quad + r;
-                    if (n >= a.N) acc[i][j][r] = -INFINITY;
-                    else if (n == t) a.hit[m] = acc[i][j][r];
-                    top = fmaxf(top, acc[i][j][r]);
-                }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float base = top == -INFINITY ? 0.f : top;  // (nothing but -inf: the sum is 0)
-            float sum = 0.f;
-#pragma unroll
-            for (int j = 0; j < FN; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) sum += __expf(acc[i][j][r] - base);
-            sum += __shfl_xor(sum, 16);
-            sum += __shfl_xor(sum, 32);
-            if (lane < 16) both[wn * BM + (wm * FM + i) * 16 + row] = make_float2(top, sum);
-        }
-        __syncthreads();
-        for (int r = threadIdx.x; r < BM; r += W * 64) {
-            float2 v = both[r];
-#pragma unroll
-            for (int q = 1; q < WN; ++q) {
-                const float2 o = both[q * BM + r];
-                const float top = fmaxf(v.x, o.x), base = top == -INFINITY ? 0.f : top;
-                v = make_float2(top, v.y * __expf(v.x - base) + o.y * __expf(o.x - base));
+            for (int j = 0; j < FN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+        // A step's second half is read while its first is multiplied; then the next step has landed, this
+        // one's buffer is free for the step after it, and the next step's first half is read while
+        // the second half is multiplied.
+        if (first < last) {
+            Frags even, odd;
+            if (first + 1 < last) landed_and_met<TP::kLoads + TQ::kLoads>();
+            else landed_and_met<0>();
+            read(even, first, 0);
+            for (int s = first; s + 1 < last; ++s) {
+                read(odd, s, 1);
+                multiply(even);
+                interleave();
+                landed_and_met<0>();
+                if (s + 2 < last) stage(s + 2);
+                read(even, s + 1, 0);
+                multiply(odd);
+                interleave();
             }
-            if (m0 + r < count) a.part[tn * a.part_ld + m0 + r] = v;
+            read(odd, last - 1, 1);
+            multiply(even);
+            multiply(odd);
         }
-    } else if constexpr (END == kGrad) {
-        T *G = static_cast<T *>(a.G);
+
+        const long m_at = m0, n_at = n0;
+        const int tn_at = tn, split_at = split;
+        landed_and_met<0>();                                 // (the row values too, where there was no step)
+        u += gridDim.x;
+        const bool more = u < units;
+        if (more) {
+            place(u);
+            stage_first(parity ^ 1);
+        }
+
+        // A lane holds, of each 16x16 tile, row lane & 15 and the four columns from 4 (lane >> 4) on.
+        int own = lane;
+        asm volatile("" : "+v"(own));
+        const int row = own & 15, quad = (own >> 4) * 4;
+        const int *targets = reinterpret_cast<const int *>(row_values + parity * 3 * BM * 4);
+        const float *lses = reinterpret_cast<const float *>(targets) + BM, *coefs = lses + BM;
+        if constexpr (END == kStats) {
+            const bool edge = n_at + BN > a.N;
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const long m = m0 + (wm * FM + i) * 16 + row;
-            const bool live = m < count;
-            const int t = live ? a.target[m] - a.n0 : -1;
-            const float lse = live ? a.lse[m] : 0.f, coef = live ? a.coef[m] : 0.f;
+            for (int i = 0; i < FM; ++i) {
+                const int lm = (wm * FM + i) * 16 + row;
+                const long m = m_at + lm;
+                const int rel = targets[lm] - (int)n_at - wn * FN * 16 - quad;
+                const bool hit = m < count && rel >= 0 && rel < FN * 16 && (rel & 12) == 0;
+                if (__any(hit)) {
+                    float z = 0.f;
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const long n = n0 + (wn * FN + j) * 16 + quad;
-                if (n >= a.g_ld) continue;
-                float g[4];
+                    for (int j = 0; j < FN; ++j)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float p = __expf(acc[i][j][r] - lse);
-                    g[r] = live && n + r < a.N ? (p - (n + r == t ? 1.f : 0.f)) * coef : 0.f;
+                        for (int r = 0; r < 4; ++r) z = rel == j * 16 + r ? acc[i][j][r] : z;
+                    if (hit) a.hit[m] = z;
                 }
-                if (m >= a.M) continue;
-                T *to = G + m * (SPLIT ? 3 * a.g_term : a.g_ld) + n;
-                if constexpr (SPLIT) {
-                    uint2 h, l1, l2;
-                    split4(g[0], g[1], g[2], g[3], h, l1, l2);
-                    *reinterpret_cast<uint2 *>(to) = h;
-                    *reinterpret_cast<uint2 *>(to + a.g_term) = l1;
-                    *reinterpret_cast<uint2 *>(to + 2 * a.g_term) = l2;
-                } else {
-                    T v[4] = {(T)g[0], (T)g[1], (T)g[2], (T)g[3]};
-                    __builtin_memcpy(__builtin_assume_aligned(to, 8), v, 8);
+                if (edge) {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (n_at + (wn * FN + j) * 16 + quad + r >= a.N) acc[i][j][r] = -INFINITY;
+                }
+                float top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < FN; ++j) top = fmaxf(fmaxf(fmaxf(top, acc[i][j][0]), acc[i][j][1]), fmaxf(acc[i][j][2], acc[i][j][3]));
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float base = top == -INFINITY ? 0.f : top;  // (nothing but -inf: the sum is 0)
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sum += __expf(acc[i][j][r] - base);
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
+                if (lane < 16) both[wn * BM + lm] = make_float2(top, sum);
+            }
+            lds_written_and_met();
+            for (int r = threadIdx.x; r < BM; r += W * 64) {
+                float2 v = both[r];
+#pragma unroll
+                for (int q = 1; q < WN; ++q) {
+                    const float2 o = both[q * BM + r];
+                    const float top = fmaxf(v.x, o.x), base = top == -INFINITY ? 0.f : top;
+                    v = make_float2(top, v.y * __expf(v.x - base) + o.y * __expf(o.x - base));
+                }
+                if (m_at + r < count) a.part[tn_at * a.part_ld + m_at + r] = v;
+            }
+        } else if constexpr (END == kGrad) {
+            T *G = static_cast<T *>(a.G);
+            const bool edge = n_at + BN > a.N || m_at + BM > count;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const int lm = (wm * FM + i) * 16 + row;
+                const long m = m_at + lm;
+                const int rel = targets[lm] - a.n0 - (int)n_at - wn * FN * 16 - quad;
+                const float lse = lses[lm], coef = coefs[lm];
+                const bool hit = m < count && rel >= 0 && rel < FN * 16 && (rel & 12) == 0;
+                const bool any = __any(hit);
+                T *to = G + m * (SPLIT ? 3 * a.g_term : a.g_ld) + n_at + wn * FN * 16 + quad;
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    float g[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) g[r] = __expf(acc[i][j][r] - lse);
+                    if (any)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) g[r] -= hit && rel == j * 16 + r ? 1.f : 0.f;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) g[r] *= coef;
+                    if (edge) {
+                        const long n = n_at + (wn * FN + j) * 16 + quad;
+                        if (m >= a.M || n >= a.g_ld) continue;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) g[r] = m < count && n + r < a.N ? g[r] : 0.f;
+                    }
+                    if constexpr (SPLIT) {
+                        uint2 h, l1, l2;
+                        split4(g[0], g[1], g[2], g[3], h, l1, l2);
+                        *reinterpret_cast<uint2 *>(to + j * 16) = h;
+                        *reinterpret_cast<uint2 *>(to + j * 16 + a.g_term) = l1;
+                        *reinterpret_cast<uint2 *>(to + j * 16 + 2 * a.g_term) = l2;
+                    } else {
+                        T v[4] = {(T)g[0], (T)g[1], (T)g[2], (T)g[3]};
+                        __builtin_memcpy(__builtin_assume_aligned(to + j * 16, 8), v, 8);
+                    }
+                }
+            }
+        } else {
+            const float alpha = a.partial ? 1.f : *a.alpha_scale;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const long m = m_at + (wm * FM + i) * 16 + row;
+                if (m >= a.M || (END == kRows && m >= count)) continue;
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    const long n = n_at + (wn * FN + j) * 16 + quad;
+                    if (n >= a.N) continue;
+                    floatx4 v = acc[i][j];
+                    if (a.partial) {
+                        floatx4 *to = reinterpret_cast<floatx4 *>(a.partial + ((size_t)split_at * a.M + m) * a.part_cols + n);
+                        *to = a.add ? *to + v : v;           // (part_cols is a multiple of four)
+                    } else {
+                        const int left = (int)(a.N - n);
+                        auto put = [&](auto *out) {
+                            typedef typename std::remove_pointer<decltype(out)>::type O;
+                            out += m * a.out_ld + n;
+                            float f[4];
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) f[r] = v[r] * alpha;
+                            if (a.add)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) if (r < left) f[r] += to_float(out[r]);
+                            O t[4] = {(O)f[0], (O)f[1], (O)f[2], (O)f[3]};
+                            if (left >= 4) __builtin_memcpy(out, t, sizeof(t));
+                            else
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) if (r < left) out[r] = t[r];
+                        };
+                        if constexpr (SPLIT) put(static_cast<float *>(a.out));
+                        else put(static_cast<T *>(a.out));
+                    }
                 }
             }
         }
-    } else {
-        const float alpha = a.partial ? 1.f : a.alpha * *a.alpha_scale;
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const long m = m0 + (wm * FM + i) * 16 + row;
-            if (m >= a.M || (END == kRows && m >= count)) continue;
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const long n = n0 + (wn * FN + j) * 16 + quad;
-                if (n >= a.N) continue;
-                floatx4 v = acc[i][j];
-                if (a.partial) {
-                    floatx4 *to = reinterpret_cast<floatx4 *>(a.partial + ((size_t)split * a.M + m) * a.part_cols + n);
-                    *to = a.add ? *to + v : v;               // (part_cols is a multiple of four)
-                } else {
-                    const int left = (int)(a.N - n);
-                    auto put = [&](auto *out) {
-                        typedef typename std::remove_pointer<decltype(out)>::type O;
-                        out += m * a.out_ld + n;
-                        float f[4];
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) f[r] = v[r] * alpha;
-                        if (a.add)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) if (r < left) f[r] += to_float(out[r]);
-                        O t[4] = {(O)f[0], (O)f[1], (O)f[2], (O)f[3]};
-                        if (left >= 4) __builtin_memcpy(out, t, sizeof(t));
-                        else
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) if (r < left) out[r] = t[r];
-                    };
-                    if constexpr (SPLIT) put(static_cast<float *>(a.out));
-                    else put(static_cast<T *>(a.out));
-                }
-            }
-        }
+        if (!more) return;
+        parity ^= 1;
     }
 }
 

@@ -308,6 +308,7 @@ __global__ __launch_bounds__(kThreads) void xent_classes_out_kernel(ClassesOutAr
 
 // ---------------------------------------------------------------------------------- plan
 struct Shape { int big, tiles_m, tiles_n, splits; };
+constexpr long kBigPlaces = 256, kSmallPlaces = 512;     // blocks the chip holds at once
 
 // 256x256 tiles where they fill the chip (one block a CU), 128x128 ones (two a CU) where they do not.
 // Where the reduction may be split, it is, until there is a block for every place.
@@ -321,7 +322,7 @@ Shape shape_of(long M, long N, long K, bool split) {
     s.tiles_n = (int)(s.big ? n2 : n1);
     s.splits = 1;
     if (split) {
-        const long tiles = (long)s.tiles_m * s.tiles_n, places = s.big ? 256 : 512;
+        const long tiles = (long)s.tiles_m * s.tiles_n, places = s.big ? kBigPlaces : kSmallPlaces;
         long want = places / tiles;
         if (want > most) want = most;
         if (want > 64) want = 64;
@@ -352,7 +353,7 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at = up(at + bytes, 256); return o; };
     p.row_of = take((size_t)N * 4);
-    p.target = take((size_t)N * 4);
+    p.target = take((size_t)p.Np * 4);                   // (the products read the rows' values a tile at a time)
     p.count = take(32);                                  // count, alpha, and from 16 on zeros
     p.x = take((size_t)p.Np * p.terms * p.Dp * 2);
     p.w = take(p.pack_w ? (size_t)V * p.terms * p.Dp * 2 : 0);
@@ -362,8 +363,8 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
         p.part = take((size_t)p.score.tiles_n * p.Np * 8);
     } else {
         p.pos = take((size_t)N * 4);
-        p.lse = take((size_t)N * 4);
-        p.coef = take((size_t)N * 4);
+        p.lse = take((size_t)p.Np * 4);
+        p.coef = take((size_t)p.Np * 4);
         long most = (long)(kPieceBytes / ((size_t)p.Np * 2 * p.terms)) / 256 * 256;
         if (most < 2048) most = 2048;
         p.pieces = (int)(((long)V + most - 1) / most);
@@ -384,17 +385,17 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
 template <class T, int END, bool SPLIT>
 hipError_t product(GemmArgs &g, const Shape &sh, hipStream_t s) {
     g.tiles_m = sh.tiles_m; g.tiles_n = sh.tiles_n; g.splits = sh.splits;
-    const long blocks = (long)sh.tiles_m * sh.tiles_n * sh.splits;
-    if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks);
+    const long tiles = (long)sh.tiles_m * sh.tiles_n * sh.splits, places = sh.big ? kBigPlaces : kSmallPlaces;
+    if (tiles > 0x7fffffffL) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)(tiles < places ? tiles : places));
     if (sh.big) {
         auto k = xent_gemm_kernel<T, 4, 8, 4, 2, END, SPLIT>;
-        constexpr int lds = 2 * 512 * 128;
+        constexpr int lds = xent_lds_bytes(256, 256, 2);
         if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(k), lds); e != hipSuccess) return e;
         hipLaunchKernelGGL(k, grid, dim3(512), lds, s, g);
     } else {
         auto k = xent_gemm_kernel<T, 4, 4, 2, 2, END, SPLIT>;
-        constexpr int lds = 2 * 256 * 128;
+        constexpr int lds = xent_lds_bytes(128, 128, 2);
         if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(k), lds); e != hipSuccess) return e;
         hipLaunchKernelGGL(k, grid, dim3(256), lds, s, g);
     }
@@ -490,7 +491,7 @@ struct Xent {
                 r.count = sc.count; r.zeros = zeros();
                 r.M = (int)p.Np; r.N = c.D; r.K = width;
                 r.partial = at<float>(p.gx); r.part_cols = p.Dc; r.add = i > 0;
-                r.alpha_scale = sc.alpha; r.alpha = 1.f;
+                r.alpha_scale = sc.alpha;
                 if (hipError_t e = product<T, kRows, SPLIT>(r, p.rows, s); e != hipSuccess) return e;
             }
             if (c.gw) {
@@ -498,7 +499,7 @@ struct Xent {
                 w.P = G; w.Q = features();
                 w.count = sc.count; w.zeros = zeros();
                 w.M = width; w.N = c.D; w.K = (int)c.N;
-                w.alpha_scale = sc.alpha; w.alpha = 1.f;
+                w.alpha_scale = sc.alpha;
                 S *gw = static_cast<S *>(c.gw) + v0 * c.D;
                 const Shape sh = tiles(p.classes, width, c.D);
                 if (sh.splits > 1) { w.partial = at<float>(p.gw); w.part_cols = p.Dc; }
