@@ -114,23 +114,27 @@ __global__ __launch_bounds__(kThreads) void planes_to_rows_kernel(TurnArgs<T> a)
 }
 
 // ---------------------------------------------------------------------------------- sort
-constexpr int kDigitBits = 10, kDigits = 1 << kDigitBits;
-constexpr int kMaxBlocks = 512;
+// Least significant digit first, stable.  A block places 1024 neighbouring items; where each digit of
+// a block begins follows from the counts of all items and of those before the block.
+//  - Up to kShort items each block counts them all itself: one launch a digit, which is what short lists
+//    cost (a launch takes 4 to 5 us however little it does: five of them 51 us for 16384 items).
+//  - Longer lists are counted by block in a launch of their own, and a launch turns counts into places.
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
+constexpr int kItems = 1024;
+constexpr long kShort = 65536;
 
 struct SortPlan {
     int passes, bits;     // digits, bits of one
     int blocks;
-    long items;           // per block, a multiple of 256
 };
 SortPlan sort_plan(long N, int V) {
     int bits = 1;
     while (bits < 31 && (1L << bits) < V) ++bits;
     SortPlan p;
     p.passes = (bits + kDigitBits - 1) / kDigitBits;
+    if (p.passes < 2) p.passes = 2;      // the first clears what the last one sets (`present`)
     p.bits = (bits + p.passes - 1) / p.passes;
-    p.items = ceil_to((N + kMaxBlocks - 1) / kMaxBlocks, kThreads);
-    if (p.items < 1024) p.items = 1024;
-    p.blocks = (int)((N + p.items - 1) / p.items);
+    p.blocks = (int)((N + kItems - 1) / kItems);
     return p;
 }
 
@@ -138,117 +142,151 @@ struct SortArgs {
     Tokens tok;               // the first pass reads these,
     const int *key_in, *idx_in;   // the others these
     int *key_out, *idx_out;
-    int *hist;                // [blocks][digits]
+    int *hist, *totals;       // [blocks][digits] and [digits]: counts, then places; null for short lists
     int *count;               // how many rows have a token
-    unsigned char *present;   // [V], first pass; null where nobody asks
-    long N, items;
+    unsigned char *present;   // [V], cleared by the first launch, set by the last; null where nobody asks
+    long N;
     int V, shift, bits, blocks;
-    int first;
+    int first, last;
 };
 
-__device__ __forceinline__ bool sort_item(const SortArgs &a, long at, long end, int &key, int &idx) {
-    key = -1; idx = 0;
-    if (at < end) {
-        if (a.first) { key = a.tok(at); idx = (int)at; }
-        else { key = a.key_in[at]; idx = a.idx_in[at]; }
-    }
-    return key >= 0;
+__device__ __forceinline__ int sort_key(const SortArgs &a, long at, long n) {
+    return at < n ? a.first ? a.tok(at) : a.key_in[at] : -1;
+}
+__device__ __forceinline__ void clear_present(const SortArgs &a, int threads) {
+    if (a.first && a.present)
+        for (long v = (long)blockIdx.x * threads + threadIdx.x; v < a.V; v += (long)gridDim.x * threads) a.present[v] = 0;
+}
+
+// Adds a wave's digits to counts.  Text is made of few tokens: the digit of the first lane that has one is
+// counted by all lanes at once, the others by an atomic each.
+__device__ __forceinline__ void count_digits(int *h, bool has, int digit) {
+    const unsigned long long any = __ballot(has);
+    if (!any) return;
+    const int common = __builtin_amdgcn_readlane(digit, __ffsll(any) - 1);
+    const unsigned long long same = __ballot(has && digit == common);
+    if (has && digit != common) atomicAdd(&h[digit], 1);
+    if ((threadIdx.x & 63) == 0) atomicAdd(&h[common], __popcll(same));
 }
 
 __global__ __launch_bounds__(kThreads) void sort_count_kernel(SortArgs a) {
     __shared__ int h[kDigits];
-    const int nd = 1 << a.bits;
-    for (int d = threadIdx.x; d < nd; d += kThreads) h[d] = 0;
-    if (a.first && a.present)
-        for (long v = (long)blockIdx.x * kThreads + threadIdx.x; v < a.V; v += (long)gridDim.x * kThreads) a.present[v] = 0;
+    const int nd = 1 << a.bits, tid = threadIdx.x;
+    for (int d = tid; d < nd; d += kThreads) h[d] = 0;
+    clear_present(a, kThreads);
     __syncthreads();
-    const long n = a.first ? a.N : (long)*a.count;
-    const long begin = blockIdx.x * a.items, end = begin + a.items < n ? begin + a.items : n;
-    for (long at = begin + threadIdx.x; at < end; at += kThreads) {
-        int key, idx;
-        if (sort_item(a, at, end, key, idx)) atomicAdd(&h[(key >> a.shift) & (nd - 1)], 1);
+    const long begin = (long)blockIdx.x * kItems, n = a.first ? a.N : (long)*a.count;
+#pragma unroll
+    for (int i = 0; i < kItems / kThreads; ++i) {
+        const int key = sort_key(a, begin + i * kThreads + tid, n);
+        count_digits(h, key >= 0, (key >> a.shift) & (nd - 1));
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < nd; d += kThreads) a.hist[(size_t)blockIdx.x * nd + d] = h[d];
+    for (int d = tid; d < nd; d += kThreads) a.hist[(size_t)blockIdx.x * nd + d] = h[d];
 }
 
-// Every block finds its own place for each digit from all blocks' counts, then places its items in
-// order: a wave takes a contiguous piece, 64 items at a time, and within those a lane's rank is
-// the number of lower lanes with the same digit.
-__global__ __launch_bounds__(kThreads) void sort_place_kernel(SortArgs a) {
-    __shared__ int base[kDigits];
-    __shared__ int mine[kWaves][kDigits];
-    __shared__ int part[kThreads];
-    const int nd = 1 << a.bits, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int per = (nd + kThreads - 1) / kThreads;     // neighbouring digits per thread
+// Counts to places, by digit: 64 digits a block, 16 threads walk the blocks of one.
+__global__ __launch_bounds__(1024) void sort_columns_kernel(SortArgs a) {
+    __shared__ int sums[16][64];
+    const int nd = 1 << a.bits, lane = threadIdx.x & 63, w = threadIdx.x >> 6, d = blockIdx.x * 64 + lane;
+    const int each = (a.blocks + 15) / 16, from = w * each, to = from + each < a.blocks ? from + each : a.blocks;
     int sum = 0;
-    for (int i = 0; i < per; ++i) {
-        const int d = tid * per + i;
-        int all = 0, before = 0;
-        if (d < nd)
-            for (int b = 0; b < a.blocks; ++b) {
-                const int h = a.hist[(size_t)b * nd + d];
-                all += h;
-                before += b < (int)blockIdx.x ? h : 0;
-            }
-        if (d < nd) { base[d] = before + sum; sum += all; }
-    }
-    part[tid] = sum;
-    for (int d = tid; d < nd; d += kThreads)
-#pragma unroll
-        for (int q = 0; q < kWaves; ++q) mine[q][d] = 0;
+    if (d < nd)
+        for (int b = from; b < to; ++b) sum += a.hist[(size_t)b * nd + d];
+    sums[w][lane] = sum;
     __syncthreads();
-    for (int step = 1; step < kThreads; step <<= 1) {
-        const int v = tid >= step ? part[tid - step] : 0;
-        __syncthreads();
-        part[tid] += v;
-        __syncthreads();
+    int at = 0, all = 0;
+    for (int q = 0; q < 16; ++q) {
+        at += q < w ? sums[q][lane] : 0;
+        all += sums[q][lane];
     }
-    const int offset = part[tid] - sum;
-    for (int i = 0; i < per; ++i)
-        if (tid * per + i < nd) base[tid * per + i] += offset;
-    if (a.first && blockIdx.x == 0 && tid == kThreads - 1) *a.count = part[tid];
+    if (d < nd) {
+        for (int b = from; b < to; ++b) {
+            const int c = a.hist[(size_t)b * nd + d];
+            a.hist[(size_t)b * nd + d] = at;
+            at += c;
+        }
+        if (w == 0) a.totals[d] = all;
+    }
+}
 
+// One item a thread.  A lane's rank is the number of lower lanes with its digit; waves follow each
+// other by their counts.
+constexpr int kPlaceWaves = kItems / 64;
+__global__ __launch_bounds__(kItems) void sort_place_kernel(SortArgs a) {
+    __shared__ int base[kDigits];
+    __shared__ int mine[kPlaceWaves * kDigits];              // [waves][digits]; before that, counts of all and of earlier items
+    __shared__ int part[kPlaceWaves];
+    const int nd = 1 << a.bits, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const long n = a.first ? a.N : (long)*a.count;
-    const long wave_items = a.items / kWaves;
-    const long begin = blockIdx.x * a.items + w * wave_items;
-    const long stop = begin + wave_items < n ? begin + wave_items : n;
-    // how many of each digit the earlier waves of this block hold
-    for (long at = begin; at < stop; at += 64) {
-        int key, idx;
-        if (sort_item(a, at + lane, stop, key, idx)) atomicAdd(&mine[w][(key >> a.shift) & (nd - 1)], 1);
-    }
-    __syncthreads();
-    for (int d = tid; d < nd; d += kThreads) {
-        int at = base[d];
+    const long begin = (long)blockIdx.x * kItems, at = begin + tid;
+    const int key = sort_key(a, at, n), digit = (key >> a.shift) & (nd - 1);
+    const int idx = a.first || at >= n ? (int)at : a.idx_in[at];
+    const bool has = key >= 0;
+    int sum = 0, before = 0;
+    if (!a.hist) {
+        clear_present(a, kItems);
+        int *all = mine, *early = mine + kDigits;
+        for (int d = tid; d < nd; d += kItems) all[d] = early[d] = 0;
+        __syncthreads();
+        constexpr int U = 8;                                 // blocks of items read at a time
+        for (long b = 0; b * kItems < n; b += U) {
+            int k[U];
 #pragma unroll
-        for (int q = 0; q < kWaves; ++q) { const int c = mine[q][d]; mine[q][d] = at; at += c; }
+            for (int u = 0; u < U; ++u) k[u] = sort_key(a, (b + u) * kItems + tid, n);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                count_digits(b + u < (long)blockIdx.x ? early : all, k[u] >= 0, (k[u] >> a.shift) & (nd - 1));
+        }
+        __syncthreads();
+        if (tid < nd) { before = early[tid]; sum = all[tid] + before; }
+        __syncthreads();
+    } else if (tid < nd) {
+        sum = a.totals[tid];
+        before = a.hist[(size_t)blockIdx.x * nd + tid];
+    }
+    // the digits before a digit
+    int upto = sum;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int v = __shfl_up(upto, m);
+        if (lane >= m) upto += v;
+    }
+    if (lane == 63) part[w] = upto;
+    for (int i = tid; i < kPlaceWaves * nd; i += kItems) mine[i] = 0;
+    __syncthreads();
+    int offset = upto - sum, all = 0;
+#pragma unroll
+    for (int q = 0; q < kPlaceWaves; ++q) {
+        offset += q < w ? part[q] : 0;
+        all += part[q];
+    }
+    if (tid < nd) base[tid] = offset + before;
+    if (a.first && blockIdx.x == 0 && tid == 0) *a.count = all;
+    unsigned long long same = __ballot(has);
+    for (int b = 0; b < a.bits; ++b) {
+        const unsigned long long set = __ballot((digit >> b) & 1);
+        same &= (digit >> b) & 1 ? set : ~set;
+    }
+    const int rank = __popcll(same & ((1ull << lane) - 1));
+    if (has && rank == 0) mine[w * nd + digit] = __popcll(same);
+    __syncthreads();
+    if (tid < nd) {
+        int to = base[tid];
+        for (int q = 0; q < kPlaceWaves; ++q) { const int c = mine[q * nd + tid]; mine[q * nd + tid] = to; to += c; }
     }
     __syncthreads();
-    for (long at = begin; at < stop; at += 64) {
-        int key, idx;
-        const bool has = sort_item(a, at + lane, stop, key, idx);
-        const int digit = (key >> a.shift) & (nd - 1);
-        unsigned long long same = __ballot(has);
-        for (int b = 0; b < a.bits; ++b) {
-            const unsigned long long set = __ballot((digit >> b) & 1);
-            same &= (digit >> b) & 1 ? set : ~set;
-        }
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        int place = 0;
-        if (has) place = mine[w][digit] + rank;
-        __builtin_amdgcn_wave_barrier();
-        if (has && rank == 0) mine[w][digit] += __popcll(same);
-        __builtin_amdgcn_wave_barrier();
-        if (has) {
-            a.key_out[place] = key;
-            a.idx_out[place] = idx;
-            if (a.first && a.present) a.present[key] = 1;
-        }
+    if (has) {
+        const int place = mine[w * nd + digit] + rank;
+        a.key_out[place] = key;
+        a.idx_out[place] = idx;
+        if (a.last && a.present) a.present[key] = 1;
     }
 }
 
 // ---------------------------------------------------------------------------------- sums
+constexpr int kMostChunk = 64;
+
 template <class T>
 struct SumArgs {
     const T *gy;
@@ -295,38 +333,42 @@ __global__ __launch_bounds__(kThreads) void embedding_sum_kernel(SumArgs<T> a) {
         }
         return;
     }
-    const long groups = kThreads / a.lanes;
-    const long unit = blockIdx.x * groups + tid / a.lanes;
+    // the chunk's tokens and rows first, so that its rows can be asked for at once
+    __shared__ int keys[kThreads * kMostChunk / 8], rows[kThreads * kMostChunk / 8];
+    const int groups = kThreads / a.lanes, g = tid / a.lanes, l = tid % a.lanes;
+    const long unit = (long)blockIdx.x * groups + g;
     const long chunk = unit / a.slices;
-    const int d = ((int)(unit - chunk * a.slices) * a.lanes + tid % a.lanes) * 8, n = a.D - d;
+    const int d = ((int)(unit - chunk * a.slices) * a.lanes + l) * 8, n = a.D - d;
     const long cnt = *a.count, begin = chunk * a.C;
-    if (begin >= cnt || n <= 0) return;
-    const long end = begin + a.C < cnt ? begin + a.C : cnt;
-    const int before = begin > 0 ? a.key[begin - 1] : -1, after = end < cnt ? a.key[end] : -1;
-    int key = a.key[begin];
+    const int len = (int)(begin + a.C < cnt ? a.C : cnt > begin ? cnt - begin : 0);
+    int *const key_of = keys + g * a.C, *const row_of = rows + g * a.C;
+    for (int i = l; i < len; i += a.lanes) {
+        key_of[i] = a.key[begin + i];
+        row_of[i] = a.idx[begin + i];
+    }
+    const int before = begin > 0 && len ? a.key[begin - 1] : -1, after = begin + len < cnt && len ? a.key[begin + len] : -1;
+    __syncthreads();
+    if (len == 0 || n <= 0) return;
+    int key = key_of[0];
     float acc[8] = {};
-    constexpr int U = 4;
-    for (long p = begin; p < end; p += U) {
-        float row[U][8];
-        int k[U];
+    constexpr int U = 8;
+    for (int p = 0; p < len; p += U) {
+        T row[U][8];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw8(a.gy + (size_t)row_of[p + u < len ? p + u : len - 1] * a.D + d, n, row[u]);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const long at = p + u < end ? p + u : end - 1;
-            k[u] = a.key[at];
-            load8(a.gy + (size_t)a.idx[at] * a.D + d, n, row[u]);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (p + u >= end) break;
-            if (k[u] != key) {
+            if (p + u >= len) break;
+            const int k = key_of[p + u];
+            if (k != key) {
                 if (key == before) store8(a.head + (size_t)chunk * a.D + d, n, acc);
                 else finish_row(a, key, d, n, acc);
-                key = k[u];
+                key = k;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) acc[i] = 0.f;
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc[i] += row[u][i];
+            for (int i = 0; i < 8; ++i) acc[i] += to_float(row[u][i]);
         }
     }
     if (key == before) store8(a.head + (size_t)chunk * a.D + d, n, acc);
@@ -334,7 +376,8 @@ __global__ __launch_bounds__(kThreads) void embedding_sum_kernel(SumArgs<T> a) {
     else finish_row(a, key, d, n, acc);
 }
 
-// One block for each chunk in which a run begins that the chunk does not end.
+// Joins the parts of the runs that cross chunks: a block for each chunk in which a run begins that the
+// chunk does not end (the others end at once).
 template <class T>
 __global__ __launch_bounds__(kThreads) void embedding_join_kernel(SumArgs<T> a) {
     __shared__ float sums[kThreads][9];
@@ -342,12 +385,11 @@ __global__ __launch_bounds__(kThreads) void embedding_join_kernel(SumArgs<T> a) 
     if (end >= cnt) return;                              // (nothing after it)
     const int key = a.key[end - 1];
     if (a.key[end] != key || (begin > 0 && a.key[begin - 1] == key)) return;
-    long lo = end, hi = cnt;                             // the run's end: the first position behind it
-    while (lo < hi) {
-        const long mid = (lo + hi) / 2;
-        if (a.key[mid] == key) lo = mid + 1; else hi = mid;
+    long last = chunk;                                   // the chunk it ends in: the last that begins with its token
+    for (int more = kThreads; more == kThreads; last += more) {      // (all ask at once: a search is a chain of reads, 10 us of them)
+        const long at = (last + 1 + threadIdx.x) * a.C;
+        more = __syncthreads_count(at < cnt && a.key[at] == key);
     }
-    const long last = (lo - 1) / a.C;                    // the chunk it ends in
     const int groups = kThreads / a.lanes, g = threadIdx.x / a.lanes, l = threadIdx.x % a.lanes;
     // group g adds the parts of a stretch of neighbouring chunks, then the stretches are added in order
     const long parts = last - chunk + 1, each = (parts + groups - 1) / groups;
@@ -355,19 +397,28 @@ __global__ __launch_bounds__(kThreads) void embedding_join_kernel(SumArgs<T> a) 
     for (int s = 0; s < a.slices; ++s) {
         const int d = (s * a.lanes + l) * 8, n = a.D - d;
         float acc[8] = {};
-        if (n > 0)
-            for (long c = from; c < to; ++c) {
-                float f[8];
-                load8((c == chunk ? a.tail : a.head) + (size_t)c * a.D + d, n, f);
+        if (n > 0) {
+            constexpr int U = 8;
+            for (long c = from; c < to; c += U) {
+                float f[U][8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[i] += f[i];
+                for (int u = 0; u < U; ++u) {
+                    const long at = c + u < to ? c + u : to - 1;
+                    load8((at == chunk ? a.tail : a.head) + (size_t)at * a.D + d, n, f[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (c + u < to)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) acc[i] += f[u][i];
             }
+        }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 8; ++i) sums[threadIdx.x][i] = acc[i];
         __syncthreads();
         if (g == 0 && n > 0) {
-            for (int q = 1; q < groups; ++q)
+            for (int q = 1; q * each < parts; ++q)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) acc[i] += sums[q * a.lanes + l][i];
             finish_row(a, key, d, n, acc);
@@ -375,11 +426,16 @@ __global__ __launch_bounds__(kThreads) void embedding_join_kernel(SumArgs<T> a) 
     }
 }
 
+template <class T>
+__global__ __launch_bounds__(kThreads) void zero_kernel(T *p, size_t n) {
+    for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (size_t)gridDim.x * kThreads) p[i] = (T)0.f;
+}
+
 struct GradPlan {
     SortPlan sort;
     int lanes, slices, C;
     long chunks;
-    size_t rows, key[2], idx[2], hist, count, present, head, tail, total;
+    size_t rows, key[2], idx[2], hist, totals, count, present, head, tail, total;
 };
 GradPlan grad_plan(int dtype, long N, int D, int V, int T) {
     GradPlan p;
@@ -387,16 +443,18 @@ GradPlan grad_plan(int dtype, long N, int D, int V, int T) {
     const int cpr = (D + 7) / 8;
     p.lanes = 1;
     while (p.lanes < cpr && p.lanes < kThreads) p.lanes *= 2;
+    if (p.lanes < 8) p.lanes = 8;
     p.slices = (cpr + p.lanes - 1) / p.lanes;
-    // chunks short enough for 64k threads, long enough that the parts they leave are few
-    const long c = N * (long)cpr / 65536;
-    p.C = (int)(c < 8 ? 8 : c > 64 ? 64 : c);
+    // chunks short enough for 128k threads, long enough that the parts they leave are few
+    const long c = N * (long)cpr / 131072;
+    p.C = (int)(c < 16 ? 16 : c > kMostChunk ? kMostChunk : c);
     p.chunks = (N + p.C - 1) / p.C;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at = up(at + bytes, 256); return o; };
     p.rows = take(T ? (size_t)N * D * type_bytes(dtype) : 0);
     for (int i = 0; i < 2; ++i) { p.key[i] = take((size_t)N * 4); p.idx[i] = take((size_t)N * 4); }
-    p.hist = take((size_t)p.sort.blocks * (4u << p.sort.bits));
+    p.hist = take(N > kShort ? (size_t)p.sort.blocks * (4u << p.sort.bits) : 0);
+    p.totals = take(4u << p.sort.bits);
     p.count = take(4);
     p.present = take(V);
     p.head = take((size_t)p.chunks * D * 4);
@@ -437,19 +495,22 @@ hipError_t accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, 
     }
     SortArgs so{};
     so.tok = tok;
-    so.hist = reinterpret_cast<int *>(ws + p.hist);
     so.count = reinterpret_cast<int *>(ws + p.count);
     so.present = accumulate ? nullptr : reinterpret_cast<unsigned char *>(ws + p.present);
-    so.N = N; so.items = p.sort.items; so.V = V; so.bits = p.sort.bits; so.blocks = p.sort.blocks;
+    so.N = N; so.V = V; so.bits = p.sort.bits; so.blocks = p.sort.blocks;
+    if (N > kShort) { so.hist = reinterpret_cast<int *>(ws + p.hist); so.totals = reinterpret_cast<int *>(ws + p.totals); }
     for (int i = 0; i < p.sort.passes; ++i) {
-        so.first = i == 0;
+        so.first = i == 0; so.last = i + 1 == p.sort.passes;
         so.shift = i * p.sort.bits;
         so.key_in = reinterpret_cast<int *>(ws + p.key[(i + 1) & 1]);
         so.idx_in = reinterpret_cast<int *>(ws + p.idx[(i + 1) & 1]);
         so.key_out = reinterpret_cast<int *>(ws + p.key[i & 1]);
         so.idx_out = reinterpret_cast<int *>(ws + p.idx[i & 1]);
-        hipLaunchKernelGGL(sort_count_kernel, dim3(so.blocks), dim3(kThreads), 0, s, so);
-        hipLaunchKernelGGL(sort_place_kernel, dim3(so.blocks), dim3(kThreads), 0, s, so);
+        if (so.hist) {
+            hipLaunchKernelGGL(sort_count_kernel, dim3(so.blocks), dim3(kThreads), 0, s, so);
+            hipLaunchKernelGGL(sort_columns_kernel, dim3(((1 << so.bits) + 63) / 64), dim3(1024), 0, s, so);
+        }
+        hipLaunchKernelGGL(sort_place_kernel, dim3(so.blocks), dim3(kItems), 0, s, so);
     }
     SumArgs<T> a{};
     a.gy = rows;
@@ -466,14 +527,8 @@ hipError_t accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, 
     const long zero_blocks = accumulate ? 0 : ((long)V + a.zero_rows - 1) / a.zero_rows;
     if (a.sum_blocks + zero_blocks > 0x7fffffffL) return hipErrorInvalidValue;
     hipLaunchKernelGGL(embedding_sum_kernel<T>, dim3((unsigned)(a.sum_blocks + zero_blocks)), dim3(kThreads), 0, s, a);
-    if (p.chunks > 1)
-        hipLaunchKernelGGL(embedding_join_kernel<T>, dim3((unsigned)p.chunks), dim3(kThreads), 0, s, a);
+    if (p.chunks > 1) hipLaunchKernelGGL(embedding_join_kernel<T>, dim3((unsigned)p.chunks), dim3(kThreads), 0, s, a);
     return hipGetLastError();
-}
-
-template <class T>
-__global__ __launch_bounds__(kThreads) void zero_kernel(T *p, size_t n) {
-    for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (size_t)gridDim.x * kThreads) p[i] = (T)0.f;
 }
 
 }  // namespace

@@ -18,7 +18,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kPerLaunch = 128;          // tensors in one launch's arguments (29 bytes each, of 4096)
-constexpr long kPieces = 4096, kLeast = 8192;
+constexpr long kPieces = 2048, kLeast = 8192;      // eight blocks a CU, none of them tiny
 
 struct NormArgs {
     const void *in[kPerLaunch];
@@ -101,7 +101,20 @@ __global__ __launch_bounds__(kThreads) void norm_end_kernel(const double *sums, 
 
 template <class T>
 __device__ __forceinline__ void scaled(const T *in, T *out, long n, float c) {
-    for (long i = (long)threadIdx.x * 8; i < n; i += kThreads * 8L) {
+    constexpr int U = 4;
+    long i = (long)threadIdx.x * 8;
+    for (; i + (U - 1) * kThreads * 8L + 8 <= n; i += U * kThreads * 8L) {
+        float f[U][8];
+#pragma unroll
+        for (int u = 0; u < U; ++u) load8(in + i + u * kThreads * 8L, 8, f[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[u][j] *= c;
+            store8(out + i + u * kThreads * 8L, 8, f[u]);
+        }
+    }
+    for (; i < n; i += kThreads * 8L) {
         const int m = (int)(n - i < 8 ? n - i : 8);
         float f[8];
         load8(in + i, m, f);
@@ -111,13 +124,14 @@ __device__ __forceinline__ void scaled(const T *in, T *out, long n, float c) {
     }
 }
 
+// The pieces are walked from the last one back: the end of what the norm read is still in the cache.
 __global__ __launch_bounds__(kThreads) void clip_kernel(NormArgs a) {
     __shared__ double lds[4];
     const double norm = sqrt(total(a.sums, a.pieces, lds));
     if (a.base == 0 && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
     const bool clip = norm > (double)a.max_norm && norm < 1.7e308;
     const float c = clip ? (float)((double)a.max_norm / norm) : 1.f;
-    const int p = blockIdx.x, t = tensor_of(a, p);
+    const int p = (int)(gridDim.x - 1 - blockIdx.x), t = tensor_of(a, p);
     if (!clip && a.in[t] == a.out[t]) return;
     const long from = (long)(p - a.first[t]) * a.piece;
     const long n = a.size[t] - from < a.piece ? a.size[t] - from : a.piece;

@@ -32,6 +32,13 @@ __device__ __forceinline__ void load8(const T *p, int n, float (&f)[8]) {
     }
 }
 template <class T>
+__device__ __forceinline__ void raw8(const T *p, int n, T (&t)[8]) {
+    if (n >= 8) __builtin_memcpy(t, p, sizeof(t));
+    else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = i < n ? p[i] : (T)0.f;
+}
+template <class T>
 __device__ __forceinline__ void store8(T *p, int n, const float (&f)[8]) {
     if (n >= 8) {
         T t[8];

@@ -20,7 +20,7 @@
 // A tile is staged with direct global-to-LDS loads of 16 bytes a lane, one K step ahead, in two
 // buffers.  LDS is written in lane order, so the swizzle that spreads a column of 16-byte pieces over
 // the banks is applied to the addresses that are read: piece c of row r holds what belongs to
-// c ^ (r & 7) (K inside), or c ^ (2 (r & 3) | (r & 8)) (K outside).
+// c ^ (r & 7) (K inside), or c ^ (2 (r & 3) | (r & 8)) (K outside, whole 256 bytes a row).
 #pragma once
 #include "operands.hpp"
 #include "kernels.hpp"
@@ -55,6 +55,7 @@ struct GemmArgs {
     const void *zeros;       // 16 bytes
     int M, N, K;             // what the grid covers
     int tiles_m, tiles_n, splits;
+    int places, most;        // rows: blocks the chip holds, steps-bound of the splits; they follow from the live rows
     // stats, grad
     const int *target;       // by row
     float2 *part;            // [tiles_n][part_ld]: maximum and sum of a row's scores in a tile
@@ -65,13 +66,19 @@ struct GemmArgs {
     long g_ld, g_term;
     long part_ld;
     // rows, classes
-    float *partial;          // [splits][M][part_cols], or null: straight to `out`
+    float *partial;          // [splits][M, or the rows of live tiles][part_cols], or null: straight to `out`
     long part_cols;
     int add;                 // add to what `partial` or `out` holds
     void *out;
     long out_ld;
     const float *alpha_scale;    // factor of `out`, on the device
 };
+
+// Into how many parts the rows product's reduction is split: until there is a block for every place.
+__host__ __device__ inline int rows_splits(long tiles, int places, int most) {
+    const long s = places / (tiles < 1 ? 1 : tiles);
+    return (int)(s < 1 ? 1 : s > most ? most : s);
+}
 
 __device__ __forceinline__ void lds_load16(const char *from, unsigned lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
@@ -112,7 +119,8 @@ struct Tile {
     const char *base;                                        // first row of the result's side, k = 0
     unsigned off[kLoads];                                    // the lane's bytes from there
 
-    static __device__ __forceinline__ int swizzle(int k) { return 2 * (k & 3) | (k & 8); }
+    // (rows of 384 bytes already alternate between the halves of the banks)
+    static __device__ __forceinline__ int swizzle(int k) { return kPieces % 16 == 0 ? 2 * (k & 3) | (k & 8) : (k & 2) | (k & 8) >> 1; }
     // Row (K inside) or k (K outside) and column of the lane's piece i.
     static __device__ __forceinline__ void place(int i, int w, int lane, int &r, int &c) {
         const int piece = (i * W + w) * 64 + lane;           // of 16 bytes, in LDS order
@@ -195,7 +203,8 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
     const int wm = w / WN, wn = w % WN;
     const int live_m = (count + BM - 1) / BM;
     const int tiles_m = END == kClasses || a.tiles_m < live_m ? a.tiles_m : live_m;
-    const int total = tiles_m * a.tiles_n, units = total * a.splits;
+    const int total = tiles_m * a.tiles_n;
+    const int splits = END == kRows ? rows_splits(total, a.places, a.most) : a.splits, units = total * splits;
     const int K = END == kClasses ? count : a.K, steps = (K + kStep - 1) / kStep;
     constexpr int kTerms = SPLIT ? 6 : 1;
 
@@ -216,7 +225,7 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
         tn = group * GN + in % gn;
         m0 = (long)(in / gn) * BM;
         n0 = (long)tn * BN;
-        const int each = (steps + a.splits - 1) / a.splits, begin = split * each;
+        const int each = (steps + splits - 1) / splits, begin = split * each;
         first = begin * kTerms;
         last = (steps < begin + each ? steps : begin + each) * kTerms;
         tp.begin(a.P, m0, w, lane);
@@ -380,32 +389,41 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
                 const float lse = lses[lm], coef = coefs[lm];
                 const bool hit = m < count && rel >= 0 && rel < FN * 16 && (rel & 12) == 0;
                 const bool any = __any(hit);
-                T *to = G + m * (SPLIT ? 3 * a.g_term : a.g_ld) + n_at + wn * FN * 16 + quad;
+                // Two column tiles at a time: lanes of odd sixteens trade theirs of the first tile for the second's of
+                // the sixteen before, after which a lane holds eight neighbouring columns of one of them.
+                const long m_ld = m * (SPLIT ? 3 * a.g_term : a.g_ld);
 #pragma unroll
-                for (int j = 0; j < FN; ++j) {
-                    float g[4];
+                for (int j = 0; j < FN; j += 2) {
+                    uint2 t[SPLIT ? 3 : 1][2];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) g[r] = __expf(acc[i][j][r] - lse);
-                    if (any)
+                    for (int h = 0; h < 2; ++h) {
+                        float g[4];
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) g[r] -= hit && rel == j * 16 + r ? 1.f : 0.f;
+                        for (int r = 0; r < 4; ++r) g[r] = __expf(acc[i][j + h][r] - lse);
+                        if (any)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) g[r] *= coef;
-                    if (edge) {
-                        const long n = n_at + (wn * FN + j) * 16 + quad;
-                        if (m >= a.M || n >= a.g_ld) continue;
+                            for (int r = 0; r < 4; ++r) g[r] -= hit && rel == (j + h) * 16 + r ? 1.f : 0.f;
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) g[r] = m < count && n + r < a.N ? g[r] : 0.f;
+                        for (int r = 0; r < 4; ++r) g[r] *= coef;
+                        if (edge) {
+                            const long n = n_at + (wn * FN + j + h) * 16 + quad;
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) g[r] = m < count && n + r < a.N ? g[r] : 0.f;
+                        }
+                        if constexpr (SPLIT) {
+                            split4(g[0], g[1], g[2], g[3], t[0][h], t[1][h], t[2][h]);
+                        } else {
+                            T v[4] = {(T)g[0], (T)g[1], (T)g[2], (T)g[3]};
+                            __builtin_memcpy(&t[0][h], v, 8);
+                        }
                     }
-                    if constexpr (SPLIT) {
-                        uint2 h, l1, l2;
-                        split4(g[0], g[1], g[2], g[3], h, l1, l2);
-                        *reinterpret_cast<uint2 *>(to + j * 16) = h;
-                        *reinterpret_cast<uint2 *>(to + j * 16 + a.g_term) = l1;
-                        *reinterpret_cast<uint2 *>(to + j * 16 + 2 * a.g_term) = l2;
-                    } else {
-                        T v[4] = {(T)g[0], (T)g[1], (T)g[2], (T)g[3]};
-                        __builtin_memcpy(__builtin_assume_aligned(to + j * 16, 8), v, 8);
+                    const long n = n_at + (wn * FN + j + (own >> 4 & 1)) * 16 + (own >> 5) * 8;
+                    if (edge && (m >= a.M || n >= a.g_ld)) continue;
+#pragma unroll
+                    for (int q = 0; q < (SPLIT ? 3 : 1); ++q) {
+                        const auto x = __builtin_amdgcn_permlane16_swap(t[q][0].x, t[q][1].x, false, false);
+                        const auto y = __builtin_amdgcn_permlane16_swap(t[q][0].y, t[q][1].y, false, false);
+                        *reinterpret_cast<uint4 *>(G + m_ld + q * a.g_term + n) = make_uint4(x[0], y[0], x[1], y[1]);
                     }
                 }
             }
@@ -421,7 +439,7 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
                     if (n >= a.N) continue;
                     floatx4 v = acc[i][j];
                     if (a.partial) {
-                        floatx4 *to = reinterpret_cast<floatx4 *>(a.partial + ((size_t)split_at * a.M + m) * a.part_cols + n);
+                        floatx4 *to = reinterpret_cast<floatx4 *>(a.partial + ((size_t)split_at * (END == kRows ? tiles_m * BM : a.M) + m) * a.part_cols + n);
                         *to = a.add ? *to + v : v;           // (part_cols is a multiple of four)
                     } else {
                         const int left = (int)(a.N - n);

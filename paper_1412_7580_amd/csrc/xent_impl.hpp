@@ -29,9 +29,17 @@ namespace {
 constexpr int kThreads = 256;
 
 // ---------------------------------------------------------------------------------- rows with a target
+// The rows that have a target, packed in their order: blocks of 1024 rows count theirs, then each places
+// its own behind those of the blocks before it.  (One block did both before, eight rows a thread:
+// 38 us for 15488 rows, beside 7 for the two launches.)
+constexpr int kScanRows = 1024;
+
 struct ScanArgs {
     Tokens tok;
     long N;
+    int blocks;
+    int *counts;                    // by block
+    float *tops;                    // by block: the largest |dL/dloss|
     int *row_of, *pos, *target;     // by packed row, by row, by packed row
     int *count;
     uint4 *zeros;                   // what the products read in place of columns that are not there
@@ -42,73 +50,100 @@ struct ScanArgs {
     int mean, half_range;           // half_range: G is held in fp16
 };
 
-__global__ __launch_bounds__(1024) void xent_scan_kernel(ScanArgs a) {
-    constexpr int E = 8;
-    __shared__ int waves[16];
-    __shared__ float tops[16];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    int base = 0;
-    float top = 0.f;
-    for (long n0 = 0; n0 < a.N; n0 += 1024 * E) {
-        int t[E], mine = 0;
+struct ScanRows { int t[4], mine, upto; float top; };
+__device__ __forceinline__ ScanRows scan_rows(const ScanArgs &a, long n0) {
+    ScanRows r;
+    r.mine = 0; r.top = 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const long n = n0 + tid * E + e;
-            t[e] = n < a.N ? a.tok(n) : -1;
-            mine += t[e] >= 0;
-        }
-        int upto = mine;
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const int v = __shfl_up(upto, m);
-            if (lane >= m) upto += v;
-        }
-        __syncthreads();
-        if (lane == 63) waves[w] = upto;
-        __syncthreads();
-        int at = base + upto - mine, all = 0;
-        for (int q = 0; q < 16; ++q) {
-            at += q < w ? waves[q] : 0;
-            all += waves[q];
-        }
-        base += all;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const long n = n0 + tid * E + e;
-            if (n >= a.N) break;
-            const bool has = t[e] >= 0;
-            if (a.pos) a.pos[n] = has ? at : -1;
-            if (has) {
-                a.row_of[at] = (int)n;
-                a.target[at] = t[e];
-                if (a.gloss) top = fmaxf(top, fabsf(a.gloss[n]));
-                ++at;
-            } else if (a.loss) {
-                a.loss[n] = 0.f;
-                a.lse[n] = 0.f;
-            }
-        }
+    for (int e = 0; e < 4; ++e) {
+        const long n = n0 + threadIdx.x * 4 + e;
+        r.t[e] = n < a.N ? a.tok(n) : -1;
+        r.mine += r.t[e] >= 0;
+        if (r.t[e] >= 0 && a.gloss) r.top = fmaxf(r.top, fabsf(a.gloss[n]));
     }
-    if (tid == 0) { *a.count = base; *a.zeros = make_uint4(0, 0, 0, 0); }
-    if (!a.coef) return;
+    r.upto = r.mine;
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-    if (lane == 0) tops[w] = top;
+    for (int m = 1; m < 64; m <<= 1) {
+        const int v = __shfl_up(r.upto, m);
+        if ((threadIdx.x & 63) >= m) r.upto += v;
+        r.top = fmaxf(r.top, __shfl_xor(r.top, m));
+    }
+    return r;
+}
+
+__global__ __launch_bounds__(kThreads) void xent_count_kernel(ScanArgs a) {
+    __shared__ int counts[4];
+    __shared__ float tops[4];
+    const ScanRows r = scan_rows(a, (long)blockIdx.x * kScanRows);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if (lane == 63) { counts[w] = r.upto; tops[w] = r.top; }
     __syncthreads();
-    for (int q = 0; q < 16; ++q) top = fmaxf(top, tops[q]);
-    int e = 0;
+    if (threadIdx.x == 0) {
+        a.counts[blockIdx.x] = counts[0] + counts[1] + counts[2] + counts[3];
+        a.tops[blockIdx.x] = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void xent_place_kernel(ScanArgs a) {
+    __shared__ int waves[4], before[4], all[4];
+    __shared__ float tops[4];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const long n0 = (long)blockIdx.x * kScanRows;
+    const ScanRows r = scan_rows(a, n0);
+    int b4 = 0, sum = 0;
+    float top = r.top;
+    if (a.blocks > 1)
+        for (int b = tid; b < a.blocks; b += kThreads) {
+            const int c = a.counts[b];
+            b4 += b < (int)blockIdx.x ? c : 0;
+            sum += c;
+            top = fmaxf(top, a.tops[b]);
+        }
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        b4 += __shfl_xor(b4, m);
+        sum += __shfl_xor(sum, m);
+        top = fmaxf(top, __shfl_xor(top, m));
+    }
+    if (lane == 63) { waves[w] = r.upto; before[w] = b4; all[w] = sum; tops[w] = top; }
+    __syncthreads();
+    int at = r.upto - r.mine, total = 0;
+    for (int q = 0; q < 4; ++q) {
+        at += before[q] + (q < w ? waves[q] : 0);
+        total += a.blocks > 1 ? all[q] : waves[q];
+        top = fmaxf(top, tops[q]);
+    }
+    int e2 = 0;
     if (a.half_range) {
         if (!a.gloss) top = 1.f;
-        if (top > 0.f && top < INFINITY) e = 14 - (ilogbf(top) + 1);
-        e = e < -100 ? -100 : e > 100 ? 100 : e;
+        if (top > 0.f && top < INFINITY) e2 = 14 - (ilogbf(top) + 1);
+        e2 = e2 < -100 ? -100 : e2 > 100 ? 100 : e2;
     }
-    const float up = ldexpf(1.f, e);
-    for (long c = tid; c < base; c += 1024) {
-        const int n = a.row_of[c];
-        a.lse_out[c] = a.lse_in[n];
-        a.coef[c] = (a.gloss ? a.gloss[n] : 1.f) * up;
+    const float up = ldexpf(1.f, e2);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const long n = n0 + tid * 4 + e;
+        if (n >= a.N) break;
+        const bool has = r.t[e] >= 0;
+        if (a.pos) a.pos[n] = has ? at : -1;
+        if (has) {
+            a.row_of[at] = (int)n;
+            a.target[at] = r.t[e];
+            if (a.coef) {
+                a.lse_out[at] = a.lse_in[n];
+                a.coef[at] = (a.gloss ? a.gloss[n] : 1.f) * up;
+            }
+            ++at;
+        } else if (a.loss) {
+            a.loss[n] = 0.f;
+            a.lse[n] = 0.f;
+        }
     }
-    if (tid == 0) *a.alpha = base ? ldexpf(a.mean ? a.scale / (float)base : a.scale, -e) : 0.f;
+    if (blockIdx.x == 0 && tid == 0) {
+        *a.count = total;
+        *a.zeros = make_uint4(0, 0, 0, 0);
+        if (a.alpha) *a.alpha = total ? ldexpf(a.mean ? a.scale / (float)total : a.scale, -e2) : 0.f;
+    }
 }
 
 // ---------------------------------------------------------------------------------- packing
@@ -190,6 +225,12 @@ struct LossArgs {
     float *loss, *lse;
 };
 
+// (maximum, sum of exponentials less that maximum) of two sets of scores taken together.
+__device__ __forceinline__ float2 joined(float2 x, float2 y) {
+    const float top = fmaxf(x.x, y.x), base = top == -INFINITY ? 0.f : top;
+    return make_float2(top, x.y * __expf(x.x - base) + y.y * __expf(y.x - base));
+}
+
 // 64 rows a block; sixteen threads a row join its tiles' maxima and sums.
 __global__ __launch_bounds__(1024) void xent_loss_kernel(LossArgs a) {
     __shared__ float2 both[16][64];
@@ -197,16 +238,12 @@ __global__ __launch_bounds__(1024) void xent_loss_kernel(LossArgs a) {
     const long m = (long)blockIdx.x * 64 + lane;
     if ((long)blockIdx.x * 64 >= count) return;
     float2 v = make_float2(-INFINITY, 0.f);
-    auto join = [](float2 x, float2 y) {
-        const float top = fmaxf(x.x, y.x), base = top == -INFINITY ? 0.f : top;
-        return make_float2(top, x.y * __expf(x.x - base) + y.y * __expf(y.x - base));
-    };
     if (m < count)
-        for (int t = w; t < a.tiles; t += 16) v = join(v, a.part[t * a.ld + m]);
+        for (int t = w; t < a.tiles; t += 16) v = joined(v, a.part[t * a.ld + m]);
     both[w][lane] = v;
     __syncthreads();
     if (w == 0 && m < count) {
-        for (int q = 1; q < 16; ++q) v = join(v, both[q][lane]);
+        for (int q = 1; q < 16; ++q) v = joined(v, both[q][lane]);
         const float lse = v.x + logf(v.y);
         const int n = a.row_of[m];
         a.lse[n] = lse;
@@ -216,12 +253,12 @@ __global__ __launch_bounds__(1024) void xent_loss_kernel(LossArgs a) {
 
 template <class S>
 struct RowsOutArgs {
-    const float *partial;     // [splits][M][ld]
-    const int *pos;           // by row
+    const float *partial;     // [splits][rows of live tiles][ld]
+    const int *pos, *count;   // pos: by row
     const float *alpha;
     S *gx;
-    long N, M, ld;
-    int splits, D, T_;
+    long N, ld;
+    int bm, tiles_n, places, most, D, T_;
 };
 
 template <class S>
@@ -229,9 +266,10 @@ __device__ __forceinline__ void sum8(const RowsOutArgs<S> &a, int c, int d, floa
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = 0.f;
     if (c < 0) return;
-    for (int s = 0; s < a.splits; ++s) {
+    const int tiles_m = (*a.count + a.bm - 1) / a.bm, splits = rows_splits((long)tiles_m * a.tiles_n, a.places, a.most);
+    for (int s = 0; s < splits; ++s) {
         float v[8];
-        load8(a.partial + ((size_t)s * a.M + c) * a.ld + d, a.D - d, v);
+        load8(a.partial + ((size_t)s * tiles_m * a.bm + c) * a.ld + d, a.D - d, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] += v[i];
     }
@@ -306,28 +344,227 @@ __global__ __launch_bounds__(kThreads) void xent_classes_out_kernel(ClassesOutAr
     }
 }
 
-// ---------------------------------------------------------------------------------- plan
-struct Shape { int big, tiles_m, tiles_n, splits; };
-constexpr long kBigPlaces = 256, kSmallPlaces = 512;     // blocks the chip holds at once
+// ---------------------------------------------------------------------------------- few rows
+// Up to a few tiles of rows the product is a read of the weights.  A block keeps its rows in LDS, whole, and
+// its waves walk the classes 16 at a time, from memory straight to the matrix cores: 16 bytes a lane, two
+// batches of eight loads in flight, the next tile's behind this one's, and no barrier on the way.  A lane
+// keeps the running maximum and sum of its own classes; lanes, waves and blocks are joined at the end.  Rows
+// need no packing: one without a target is zeros in LDS.  fp32 is multiplied in fp32 (16x16x4).
+template <class S> struct Thin;
+template <> struct Thin<float> {
+    typedef float frag __attribute__((ext_vector_type(4)));
+    static constexpr int k = 16;                             // of the reduction per 16 bytes of four lanes
+    static __device__ __forceinline__ floatx4 mul(frag a, frag b, floatx4 c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+        return c;
+    }
+};
+template <> struct Thin<__bf16> : Mfma<__bf16> { static constexpr int k = 32; };
+template <> struct Thin<_Float16> : Mfma<_Float16> { static constexpr int k = 32; };
 
-// 256x256 tiles where they fill the chip (one block a CU), 128x128 ones (two a CU) where they do not.
-// Where the reduction may be split, it is, until there is a block for every place.
-Shape shape_of(long M, long N, long K, bool split) {
-    const long m2 = (M + 255) / 256, n2 = (N + 255) / 256, m1 = (M + 127) / 128, n1 = (N + 127) / 128;
+constexpr int kThinThreads = 512, kThinWaves = 8;
+constexpr int kThinLds = 140 * 1024;
+
+template <class S>
+struct ThinArgs {
+    const S *x, *wt;
+    Tokens tok;
+    long N;
+    int D, V, T_, blocks;     // blocks: of one group of rows
+    float2 *part;             // [N][blocks]
+    float *hit;
+    float *loss, *lse;
+};
+
+template <class S, int NT>
+__global__ __launch_bounds__(kThinThreads, NT < 4 ? 4 : 2) void xent_thin_kernel(ThinArgs<S> a) {
+    typedef typename Thin<S>::frag F;
+    constexpr int E = 16 / sizeof(S), KS = Thin<S>::k, R = NT * 16;   // elements of 16 bytes, k of one load, rows
+    constexpr int AHEAD = 8;
+    extern __shared__ __align__(16) char lds[];
+    float2 (*const both)[R] = reinterpret_cast<float2 (*)[R]>(lds);                // [waves]
+    int *const live = reinterpret_cast<int *>(lds + kThinWaves * R * 8);
+    S *const xs = reinterpret_cast<S *>(lds + kThinWaves * R * 8 + R * 4);
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
+    const long r0 = (long)blockIdx.y * R;
+    const int steps = (a.D + KS - 1) / KS, batches = (steps + AHEAD - 1) / AHEAD, pitch = steps * KS + E;
+    const int tiles = (a.V + 15) / 16, stride = a.blocks * kThinWaves;
+
+    auto load = [&](F (&f)[AHEAD], int tile, int batch) {
+        int v = tile * 16 + (lane & 15);
+        if (v >= a.V) v = a.V - 1;
+        const S *p = a.wt + (size_t)v * a.D + batch * AHEAD * KS + g * E;
+        const int left = a.D - batch * AHEAD * KS;           // of the reduction
+        if (left >= AHEAD * KS) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) __builtin_memcpy(&f[i], p + i * KS, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                if (left >= (i + 1) * KS) __builtin_memcpy(&f[i], p + i * KS, 16);
+                else if (left > i * KS) {
+                    S t[E];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) t[e] = i * KS + g * E + e < left ? p[i * KS + e] : (S)0.f;
+                    __builtin_memcpy(&f[i], t, 16);
+                }
+            }
+        }
+    };
+    int tile = blockIdx.x * kThinWaves + w, batch = 0;
+    F now[AHEAD], next[AHEAD];
+    if (tile < tiles) load(now, tile, 0);
+
+    if (tid < R) live[tid] = r0 + tid < a.N && a.tok(r0 + tid) >= 0;
+    __syncthreads();
+    if (a.T_ == 0) {
+        const int pieces = steps * KS / E, all = R * pieces;
+        constexpr int U = 4;
+        for (int c0 = tid; c0 < all; c0 += U * kThinThreads) {
+            F f[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int c = c0 + u * kThinThreads, r = c / pieces, k = (c - r * pieces) * E;
+                f[u] = F{};
+                if (c >= all || !live[r]) continue;
+                const S *p = a.x + (size_t)(r0 + r) * a.D + k;
+                if (k + E <= a.D) __builtin_memcpy(&f[u], p, 16);
+                else {
+                    S t[E];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) t[e] = k + e < a.D ? p[e] : (S)0.f;
+                    __builtin_memcpy(&f[u], t, 16);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int c = c0 + u * kThinThreads, r = c / pieces, k = (c - r * pieces) * E;
+                if (c < all) __builtin_memcpy(__builtin_assume_aligned(&xs[r * pitch + k], 16), &f[u], 16);
+            }
+        }
+    } else {
+        const RowsOf at{a.D, a.T_};
+        for (int c = tid; c < R * steps * KS; c += kThinThreads) {
+            const int r = c % R, k = c / R;
+            xs[r * pitch + k] = live[r] && k < a.D ? a.x[at.offset(r0 + r) + (size_t)k * a.T_] : (S)0.f;
+        }
+    }
+    __syncthreads();
+
+    int target[NT];
+    float top[NT], sum[NT];
+    floatx4 acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const long n = r0 + t * 16 + (lane & 15);
+        target[t] = n < a.N ? a.tok(n) : -1;
+        top[t] = -INFINITY; sum[t] = 0.f;
+        acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    const S *const xl = xs + (lane & 15) * pitch + g * E;
+    while (tile < tiles) {
+        int next_tile = tile, next_batch = batch + 1;
+        if (next_batch == batches) { next_batch = 0; next_tile += stride; }
+        if (next_tile < tiles) load(next, next_tile, next_batch);
+        const S *const xk = xl + batch * AHEAD * KS;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (batch * AHEAD + i >= steps) break;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                F f;
+                __builtin_memcpy(&f, __builtin_assume_aligned(xk + t * 16 * pitch + i * KS, 16), 16);
+                acc[t] = Thin<S>::mul(now[i], f, acc[t]);
+            }
+        }
+        if (next_batch == 0) {
+            // a lane holds row lane & 15 of each tile of rows and the four classes from 4 (lane >> 4) on
+            const int v0 = tile * 16 + g * 4;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int rel = target[t] - v0;
+                if (rel >= 0 && rel < 4) {
+                    float z = 0.f;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z = rel == r ? acc[t][r] : z;
+                    a.hit[r0 + t * 16 + (lane & 15)] = z;
+                }
+                float high = -INFINITY;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    if (v0 + r >= a.V) acc[t][r] = -INFINITY;
+                    high = fmaxf(high, acc[t][r]);
+                }
+                const float m = fmaxf(top[t], high), base = m == -INFINITY ? 0.f : m;
+                float s = sum[t] * __expf(top[t] - base);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s += __expf(acc[t][r] - base);
+                top[t] = m; sum[t] = s;
+                acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) now[i] = next[i];
+        tile = next_tile; batch = next_batch;
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        float2 v = make_float2(top[t], sum[t]);
+        v = joined(v, make_float2(__shfl_xor(v.x, 16), __shfl_xor(v.y, 16)));
+        v = joined(v, make_float2(__shfl_xor(v.x, 32), __shfl_xor(v.y, 32)));
+        if (lane < 16) both[w][t * 16 + lane] = v;
+    }
+    __syncthreads();
+    if (tid < R && r0 + tid < a.N) {
+        float2 v = both[0][tid];
+        for (int q = 1; q < kThinWaves; ++q) v = joined(v, both[q][tid]);
+        a.part[(size_t)(r0 + tid) * a.blocks + blockIdx.x] = v;
+    }
+}
+
+template <class S>
+__global__ __launch_bounds__(kThreads) void xent_thin_loss_kernel(ThinArgs<S> a) {
+    __shared__ float2 both[4];
+    const long n = blockIdx.x;
+    if (a.tok(n) < 0) {
+        if (threadIdx.x == 0) { a.loss[n] = 0.f; a.lse[n] = 0.f; }
+        return;
+    }
+    float2 v = make_float2(-INFINITY, 0.f);
+    for (int b = threadIdx.x; b < a.blocks; b += kThreads) v = joined(v, a.part[(size_t)n * a.blocks + b]);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) v = joined(v, make_float2(__shfl_xor(v.x, m), __shfl_xor(v.y, m)));
+    if ((threadIdx.x & 63) == 0) both[threadIdx.x >> 6] = v;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        v = joined(joined(both[0], both[1]), joined(both[2], both[3]));
+        const float lse = v.x + logf(v.y);
+        a.lse[n] = lse;
+        a.loss[n] = lse - a.hit[n];
+    }
+}
+
+// ---------------------------------------------------------------------------------- plan
+struct Shape { int bm, bn, tiles_m, tiles_n, splits, most; };     // most: what the reduction's length allows of splits
+constexpr long kBigPlaces = 256, kSmallPlaces = 512;     // blocks the chip holds at once
+inline long places(const Shape &s) { return s.bm == 256 ? kBigPlaces : kSmallPlaces; }
+
+// Tiles of 256x256 where they fill the chip (one block a CU), of 128x128 (two a CU) where they do not.
+// Where the reduction may be split, it is, until there is a block for every place; such products take
+// tiles 192 columns wide where that covers the columns with less (384 columns: 97 -> 70 us for 15488 rows
+// and 1000 classes in fp32).
+inline Shape shape_of(long M, long N, long K, bool split) {
     const long steps = (K + kStep - 1) / kStep;
     Shape s{};
-    const long most = split ? steps / 8 < 1 ? 1 : steps / 8 : 1;
-    s.big = m2 * n2 * most >= 192;
-    s.tiles_m = (int)(s.big ? m2 : m1);
-    s.tiles_n = (int)(s.big ? n2 : n1);
-    s.splits = 1;
-    if (split) {
-        const long tiles = (long)s.tiles_m * s.tiles_n, places = s.big ? kBigPlaces : kSmallPlaces;
-        long want = places / tiles;
-        if (want > most) want = most;
-        if (want > 64) want = 64;
-        s.splits = (int)(want < 1 ? 1 : want);
-    }
+    s.most = split ? (int)(steps / 8 < 1 ? 1 : steps / 8 > 64 ? 64 : steps / 8) : 1;
+    const auto tiles = [](long n, long t) { return (n + t - 1) / t; };
+    s.bm = 256;
+    s.bn = split && tiles(N, 192) * 192 < tiles(N, 256) * 256 ? 192 : 256;
+    if (tiles(M, s.bm) * tiles(N, s.bn) * s.most < 192) s.bm = s.bn = 128;
+    s.tiles_m = (int)tiles(M, s.bm);
+    s.tiles_n = (int)tiles(N, s.bn);
+    s.splits = rows_splits((long)s.tiles_m * s.tiles_n, (int)places(s), s.most);
     return s;
 }
 
@@ -336,10 +573,29 @@ struct XentPlan {
     int Dp, Dc;               // features, up to a multiple of 8 and of 4
     int terms;
     bool pack_w;
+    int thin_tiles, thin_blocks, thin_lds;    // tiles of 16 rows in a block (0: not that path), blocks of a group of rows
     int piece, pieces;        // classes a piece
     Shape score, rows, classes;
-    size_t row_of, pos, target, count, lse, coef, hit, part, x, w, G, gx, gw, total;
+    int scan_blocks;
+    size_t row_of, pos, target, count, counts, tops, lse, coef, hit, part, x, w, G, gx, gw, total;
 };
+
+// Few rows: as many tiles of 16 of them as a block's LDS holds, four at most.  More groups of rows than
+// one read the weights again, which the other path's packing and narrow tiles cost too; in fp32 that path
+// also cuts and multiplies every weight six times.
+inline void thin_plan(XentPlan &p, int dtype, long N, int D, int V) {
+    const int s = (int)type_bytes(dtype), ks = dtype == kF32 ? 16 : 32;
+    const long row = (ceil_to(D, ks) + 16 / s) * s, groups_most = dtype == kF32 ? 4 : 2;
+    int t = N <= 16 ? 1 : N <= 32 ? 2 : 4;
+    while (t > 1 && t * 16 * row > kThinLds) t /= 2;
+    if (t * 16 * row > kThinLds || N > groups_most * t * 16) return;
+    p.thin_tiles = t;
+    p.thin_lds = (int)(t * 16 * (row + kThinWaves * 8 + 4));
+    const long groups = (N + t * 16 - 1) / (t * 16), waves = ((long)V + 15) / 16;
+    const long places = (p.thin_lds <= kThinLds / 2 ? 512 : 256) / groups;     // two blocks a CU, or one
+    const long want = (waves + kThinWaves - 1) / kThinWaves;
+    p.thin_blocks = (int)(want < places ? want : places);
+}
 
 constexpr size_t kPieceBytes = (size_t)256 << 20;
 
@@ -352,9 +608,19 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
     p.pack_w = dtype == kF32 || D % 8 || !aligned;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at = up(at + bytes, 256); return o; };
+    if (!backward) thin_plan(p, dtype, N, D, V);
+    if (p.thin_tiles) {
+        p.hit = take((size_t)N * 4);
+        p.part = take((size_t)p.thin_blocks * N * 8);
+        p.total = at;
+        return p;
+    }
     p.row_of = take((size_t)N * 4);
     p.target = take((size_t)p.Np * 4);                   // (the products read the rows' values a tile at a time)
     p.count = take(32);                                  // count, alpha, and from 16 on zeros
+    p.scan_blocks = (int)((N + kScanRows - 1) / kScanRows);
+    p.counts = take((size_t)p.scan_blocks * 4);
+    p.tops = take((size_t)p.scan_blocks * 4);
     p.x = take((size_t)p.Np * p.terms * p.Dp * 2);
     p.w = take(p.pack_w ? (size_t)V * p.terms * p.Dp * 2 : 0);
     if (!backward) {
@@ -375,7 +641,10 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
         p.rows = shape_of(N, D, widest, true);
         p.classes = shape_of(widest, D, N, true);
         p.G = take((size_t)p.Np * p.terms * ceil_to(widest, 64) * 2);
-        p.gx = take((size_t)p.rows.splits * p.Np * p.Dc * 4);
+        // the rows product splits by the tiles of rows that have a target: the fewer, the more parts, but never more
+        // tiles in all than places, or than one part of all rows
+        const long parts = places(p.rows) / p.rows.tiles_n;
+        p.gx = take((size_t)(parts > p.rows.tiles_m ? parts : p.rows.tiles_m) * p.rows.bm * p.Dc * 4);
         p.gw = take(p.classes.splits > 1 ? (size_t)p.classes.splits * widest * p.Dc * 4 : 0);
     }
     p.total = at;
@@ -385,21 +654,19 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
 template <class T, int END, bool SPLIT>
 hipError_t product(GemmArgs &g, const Shape &sh, hipStream_t s) {
     g.tiles_m = sh.tiles_m; g.tiles_n = sh.tiles_n; g.splits = sh.splits;
-    const long tiles = (long)sh.tiles_m * sh.tiles_n * sh.splits, places = sh.big ? kBigPlaces : kSmallPlaces;
+    g.places = (int)places(sh); g.most = sh.most;
+    const long tiles = (long)sh.tiles_m * sh.tiles_n * (END == kRows ? sh.most : sh.splits);
     if (tiles > 0x7fffffffL) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)(tiles < places ? tiles : places));
-    if (sh.big) {
-        auto k = xent_gemm_kernel<T, 4, 8, 4, 2, END, SPLIT>;
-        constexpr int lds = xent_lds_bytes(256, 256, 2);
-        if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(k), lds); e != hipSuccess) return e;
-        hipLaunchKernelGGL(k, grid, dim3(512), lds, s, g);
-    } else {
-        auto k = xent_gemm_kernel<T, 4, 4, 2, 2, END, SPLIT>;
-        constexpr int lds = xent_lds_bytes(128, 128, 2);
-        if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(k), lds); e != hipSuccess) return e;
-        hipLaunchKernelGGL(k, grid, dim3(256), lds, s, g);
-    }
-    return hipGetLastError();
+    const dim3 grid((unsigned)(tiles < g.places ? tiles : g.places));
+    const auto launch = [&](auto kernel, int threads, int lds) {
+        if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(kernel), lds); e != hipSuccess) return e;
+        hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, s, g);
+        return hipGetLastError();
+    };
+    if constexpr (END == kRows || END == kClasses)
+        if (sh.bn == 192) return launch(xent_gemm_kernel<T, 4, 6, 4, 2, END, SPLIT>, 512, xent_lds_bytes(256, 192, 2));
+    if (sh.bm == 256) return launch(xent_gemm_kernel<T, 4, 8, 4, 2, END, SPLIT>, 512, xent_lds_bytes(256, 256, 2));
+    return launch(xent_gemm_kernel<T, 4, 4, 2, 2, END, SPLIT>, 256, xent_lds_bytes(128, 128, 2));
 }
 
 inline unsigned blocks_for(size_t chunks) {
@@ -422,6 +689,13 @@ struct Xent {
     template <class P> P *at(size_t o) const { return reinterpret_cast<P *>(ws + o); }
     const void *zeros() const { return ws + p.count + 16; }
 
+    void scan(ScanArgs &sc) {
+        sc.tok = c.tok; sc.N = c.N; sc.blocks = p.scan_blocks;
+        sc.counts = at<int>(p.counts); sc.tops = at<float>(p.tops);
+        sc.row_of = at<int>(p.row_of); sc.target = at<int>(p.target); sc.count = at<int>(p.count); sc.zeros = at<uint4>(p.count + 16);
+        if (sc.blocks > 1) hipLaunchKernelGGL(xent_count_kernel, dim3(sc.blocks), dim3(kThreads), 0, s, sc);
+        hipLaunchKernelGGL(xent_place_kernel, dim3(sc.blocks), dim3(kThreads), 0, s, sc);
+    }
     hipError_t pack() {
         PackArgs<S, T, SPLIT> a{static_cast<const S *>(c.x), at<T>(p.x), at<int>(p.row_of), at<int>(p.count), p.Np, c.D, p.Dp, c.T};
         if (c.T) {
@@ -444,12 +718,24 @@ struct Xent {
         return GemmSide{w + v0 * ld, ld, p.Dp, c.V - v0, p.Dp};
     }
 
+    template <int NT>
+    hipError_t thin_tiles(const ThinArgs<S> &a) {
+        auto k = xent_thin_kernel<S, NT>;
+        if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(k), p.thin_lds); e != hipSuccess) return e;
+        hipLaunchKernelGGL(k, dim3(p.thin_blocks, (unsigned)((c.N + NT * 16 - 1) / (NT * 16))), dim3(kThinThreads), p.thin_lds, s, a);
+        hipLaunchKernelGGL(xent_thin_loss_kernel<S>, dim3((unsigned)c.N), dim3(kThreads), 0, s, a);
+        return hipGetLastError();
+    }
+    hipError_t thin() {
+        const ThinArgs<S> a{static_cast<const S *>(c.x), static_cast<const S *>(c.wt), c.tok, c.N, c.D, c.V, c.T, p.thin_blocks,
+                            at<float2>(p.part), at<float>(p.hit), c.loss, c.lse};
+        return p.thin_tiles == 1 ? thin_tiles<1>(a) : p.thin_tiles == 2 ? thin_tiles<2>(a) : thin_tiles<4>(a);
+    }
     hipError_t fprop() {
+        if (p.thin_tiles) return thin();
         ScanArgs sc{};
-        sc.tok = c.tok; sc.N = c.N;
-        sc.row_of = at<int>(p.row_of); sc.target = at<int>(p.target); sc.count = at<int>(p.count); sc.zeros = at<uint4>(p.count + 16);
         sc.loss = c.loss; sc.lse = c.lse;
-        hipLaunchKernelGGL(xent_scan_kernel, dim3(1), dim3(1024), 0, s, sc);
+        scan(sc);
         if (hipError_t e = pack(); e != hipSuccess) return e;
         GemmArgs g{};
         g.P = features(); g.Q = weights(0);
@@ -464,13 +750,12 @@ struct Xent {
 
     hipError_t backward() {
         ScanArgs sc{};
-        sc.tok = c.tok; sc.N = c.N;
-        sc.row_of = at<int>(p.row_of); sc.pos = at<int>(p.pos); sc.target = at<int>(p.target); sc.count = at<int>(p.count); sc.zeros = at<uint4>(p.count + 16);
+        sc.pos = at<int>(p.pos);
         sc.lse_in = c.lse; sc.gloss = c.gloss;
         sc.lse_out = at<float>(p.lse); sc.coef = at<float>(p.coef);
-        sc.alpha = reinterpret_cast<float *>(sc.count + 1);
+        sc.alpha = at<float>(p.count + 4);
         sc.scale = c.scale; sc.mean = c.mean; sc.half_range = c.dtype == kF16;
-        hipLaunchKernelGGL(xent_scan_kernel, dim3(1), dim3(1024), 0, s, sc);
+        scan(sc);
         if (hipError_t e = pack(); e != hipSuccess) return e;
         for (int i = 0; i < p.pieces; ++i) {
             const long v0 = (long)i * p.piece;
@@ -512,7 +797,8 @@ struct Xent {
             }
         }
         if (c.gx) {
-            const RowsOutArgs<S> o{at<float>(p.gx), sc.pos, sc.alpha, static_cast<S *>(c.gx), c.N, p.Np, p.Dc, p.rows.splits, c.D, c.T};
+            const RowsOutArgs<S> o{at<float>(p.gx), sc.pos, sc.count, sc.alpha, static_cast<S *>(c.gx), c.N, p.Dc,
+                                   p.rows.bm, p.rows.tiles_n, (int)places(p.rows), p.rows.most, c.D, c.T};
             if (c.T) {
                 const long blocks = c.N / c.T * ((c.T + 63) / 64) * ((c.D + 63) / 64);
                 if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
@@ -525,9 +811,8 @@ struct Xent {
     }
     // The last piece may be narrower than the plan's.
     static Shape tiles(Shape sh, long M, long N) {
-        const long t = sh.big ? 256 : 128;
-        sh.tiles_m = (int)((M + t - 1) / t);
-        sh.tiles_n = (int)((N + t - 1) / t);
+        sh.tiles_m = (int)((M + sh.bm - 1) / sh.bm);
+        sh.tiles_n = (int)((N + sh.bn - 1) / sh.bn);
         return sh;
     }
 };
