@@ -820,10 +820,14 @@ class Handle:
         return int(self._lib.fftconv_grad_workspace_bytes(n, (ctypes.c_long * n)(*[t.numel() for t in grads])))
 
     def _tensor_list(self, grads):
-        n = len(grads)
-        got = [self._operand(t, "a gradient") for t in grads]
-        return n, (ctypes.c_void_p * n)(*[p for p, _ in got]), (ctypes.c_long * n)(*[t.numel() for t in grads]), \
-            (ctypes.c_int * n)(*[k for _, k in got])
+        n, dev = len(grads), self.device
+        pointers, sizes, kinds = (ctypes.c_void_p * n)(), (ctypes.c_long * n)(), (ctypes.c_int * n)()
+        for i, t in enumerate(grads):
+            k = _types.get(t.dtype) if isinstance(t, torch.Tensor) else None
+            if k is None or t.get_device() != dev or not t.is_contiguous():
+                self._operand(t, "a gradient")         # says what is wrong with it
+            pointers[i], sizes[i], kinds[i] = t.data_ptr(), t.numel(), k
+        return n, pointers, sizes, kinds
 
     def _norm_result(self, norm):
         if norm is None:

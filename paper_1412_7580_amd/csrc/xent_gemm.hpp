@@ -212,13 +212,14 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
     TQ tq;
     long m0, n0;
     int tn, split, first, last;
-    // Neighbouring blocks go to different XCDs: each XCD takes a contiguous eighth of the tiles, walked
-    // in columns of four tiles so that what its L2 holds is used several times.
+    // Neighbouring blocks go to different XCDs: each XCD takes a contiguous eighth of the tiles (all of a
+    // split's before the next one's), walked in columns of four tiles so that what its L2 holds is used
+    // several times.
     auto place = [&](int u) {
-        split = u / total;
-        int id = u - split * total;
-        const int per = total / 8, more = total % 8, x = id % 8;
-        id = x * per + (x < more ? x : more) + id / 8;
+        const int per = units / 8, more = units % 8, x = u % 8;
+        int id = x * per + (x < more ? x : more) + u / 8;
+        split = id / total;
+        id -= split * total;
         constexpr int GN = 4;
         const int group = id / (GN * tiles_m), in = id - group * GN * tiles_m;
         const int gn = a.tiles_n - group * GN < GN ? a.tiles_n - group * GN : GN;
@@ -429,6 +430,31 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
             }
         } else {
             const float alpha = a.partial ? 1.f : *a.alpha_scale;
+            if constexpr (END == kClasses && !SPLIT) {
+                // straight to 16-bit weights' gradients, 16 bytes a lane where their rows allow it
+                if (!a.partial && !a.add && a.out_ld % 8 == 0 && ((unsigned long)a.out & 15) == 0 && n_at + BN <= a.N) {
+#pragma unroll
+                    for (int i = 0; i < FM; ++i) {
+                        const long m = m_at + (wm * FM + i) * 16 + row;
+                        T *to = static_cast<T *>(a.out) + m * a.out_ld + n_at + (wn * FN + (own >> 4 & 1)) * 16 + (own >> 5) * 8;
+#pragma unroll
+                        for (int j = 0; j < FN; j += 2) {
+                            uint2 t[2];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                T v[4];
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) v[r] = (T)(acc[i][j + h][r] * alpha);
+                                __builtin_memcpy(&t[h], v, 8);
+                            }
+                            const auto x = __builtin_amdgcn_permlane16_swap(t[0].x, t[1].x, false, false);
+                            const auto y = __builtin_amdgcn_permlane16_swap(t[0].y, t[1].y, false, false);
+                            if (m < a.M) *reinterpret_cast<uint4 *>(to + j * 16) = make_uint4(x[0], y[0], x[1], y[1]);
+                        }
+                    }
+                    goto done;
+                }
+            }
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
                 const long m = m_at + (wm * FM + i) * 16 + row;
@@ -464,6 +490,7 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
                 }
             }
         }
+    done:
         if (!more) return;
         parity ^= 1;
     }

@@ -29,10 +29,11 @@ namespace {
 constexpr int kThreads = 256;
 
 // ---------------------------------------------------------------------------------- rows with a target
-// The rows that have a target, packed in their order: blocks of 1024 rows count theirs, then each places
-// its own behind those of the blocks before it.  (One block did both before, eight rows a thread:
-// 38 us for 15488 rows, beside 7 for the two launches.)
-constexpr int kScanRows = 1024;
+// The rows that have a target, packed in their order: blocks of 1024 rows place theirs behind those of the
+// blocks before them.  Up to kScanInline blocks each counts all rows itself; beyond that the blocks' counts
+// come from a launch of their own.  (One block for all rows: 38 us for 15488 of them, beside 10 for two
+// launches and 7 for one.)
+constexpr int kScanRows = 1024, kScanInline = 16;
 
 struct ScanArgs {
     Tokens tok;
@@ -92,7 +93,19 @@ __global__ __launch_bounds__(kThreads) void xent_place_kernel(ScanArgs a) {
     const ScanRows r = scan_rows(a, n0);
     int b4 = 0, sum = 0;
     float top = r.top;
-    if (a.blocks > 1)
+    if (a.blocks <= kScanInline)
+        for (int b = 0; b < a.blocks; ++b) {
+            if (b == (int)blockIdx.x) { sum += r.mine; continue; }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const long n = (long)b * kScanRows + e * kThreads + tid;
+                const bool has = n < a.N && a.tok(n) >= 0;
+                b4 += has && b < (int)blockIdx.x;
+                sum += has;
+                if (has && a.gloss) top = fmaxf(top, fabsf(a.gloss[n]));
+            }
+        }
+    else
         for (int b = tid; b < a.blocks; b += kThreads) {
             const int c = a.counts[b];
             b4 += b < (int)blockIdx.x ? c : 0;
@@ -110,7 +123,7 @@ __global__ __launch_bounds__(kThreads) void xent_place_kernel(ScanArgs a) {
     int at = r.upto - r.mine, total = 0;
     for (int q = 0; q < 4; ++q) {
         at += before[q] + (q < w ? waves[q] : 0);
-        total += a.blocks > 1 ? all[q] : waves[q];
+        total += all[q];
         top = fmaxf(top, tops[q]);
     }
     int e2 = 0;
@@ -693,7 +706,7 @@ struct Xent {
         sc.tok = c.tok; sc.N = c.N; sc.blocks = p.scan_blocks;
         sc.counts = at<int>(p.counts); sc.tops = at<float>(p.tops);
         sc.row_of = at<int>(p.row_of); sc.target = at<int>(p.target); sc.count = at<int>(p.count); sc.zeros = at<uint4>(p.count + 16);
-        if (sc.blocks > 1) hipLaunchKernelGGL(xent_count_kernel, dim3(sc.blocks), dim3(kThreads), 0, s, sc);
+        if (sc.blocks > kScanInline) hipLaunchKernelGGL(xent_count_kernel, dim3(sc.blocks), dim3(kThreads), 0, s, sc);
         hipLaunchKernelGGL(xent_place_kernel, dim3(sc.blocks), dim3(kThreads), 0, s, sc);
     }
     hipError_t pack() {
