@@ -114,16 +114,20 @@ __global__ __launch_bounds__(kThreads) void planes_to_rows_kernel(TurnArgs<T> a)
 }
 
 // ---------------------------------------------------------------------------------- sort
-// Least significant digit first, stable.  A block places 1024 neighbouring items; where each digit of
-// a block begins follows from the counts of all items and of those before the block.
-//  - Up to kShort items each block counts them all itself: one launch a digit, which is what short lists
-//    cost (a launch takes 4 to 5 us however little it does: five of them 51 us for 16384 items).
-//  - Longer lists are counted by block in a launch of their own, and a launch turns counts into places.
-constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
-constexpr int kItems = 1024;
-constexpr long kShort = 65536;
+// Least significant digit first, stable.  A block's waves take neighbouring stretches of its items, 64 at a
+// time; among those a lane's rank is the number of lower lanes with its digit, found by a ballot for each bit.
+//  - Up to 4096 items one block sorts them in LDS, all digits in one launch (500 items: 5 us; 16384 of them
+//    would take 42, beside 21 for the launches of the other way).
+//  - More are sorted by blocks of 1024 with two launches a digit: counts by block, then places.  Where a
+//    digit of a block begins follows from all blocks' counts: up to kInline blocks add those up themselves,
+//    beyond that a launch turns counts into places.
+constexpr int kSortThreads = 1024, kSortWaves = 16;
+constexpr int kDigitBits = 8, kDigits = 1 << kDigitBits;
+constexpr int kOneBlock = 4096, kOneBlockClasses = 1 << 20;      // (which also clears a byte per class)
+constexpr int kItems = kSortThreads, kInline = 32;
 
 struct SortPlan {
+    bool one;
     int passes, bits;     // digits, bits of one
     int blocks;
 };
@@ -131,8 +135,9 @@ SortPlan sort_plan(long N, int V) {
     int bits = 1;
     while (bits < 31 && (1L << bits) < V) ++bits;
     SortPlan p;
+    p.one = N <= kOneBlock && V <= kOneBlockClasses;
     p.passes = (bits + kDigitBits - 1) / kDigitBits;
-    if (p.passes < 2) p.passes = 2;      // the first clears what the last one sets (`present`)
+    if (p.passes < 2 && !p.one) p.passes = 2;      // the first clears what the last one sets (`present`)
     p.bits = (bits + p.passes - 1) / p.passes;
     p.blocks = (int)((N + kItems - 1) / kItems);
     return p;
@@ -142,51 +147,154 @@ struct SortArgs {
     Tokens tok;               // the first pass reads these,
     const int *key_in, *idx_in;   // the others these
     int *key_out, *idx_out;
-    int *hist, *totals;       // [blocks][digits] and [digits]: counts, then places; null for short lists
+    int *hist, *totals;       // [blocks][digits] and [digits]: counts, or places where there are totals
     int *count;               // how many rows have a token
     unsigned char *present;   // [V], cleared by the first launch, set by the last; null where nobody asks
     long N;
-    int V, shift, bits, blocks;
-    int first, last;
+    int V, shift, bits, passes, blocks;
+    int first, last, placed;
 };
 
 __device__ __forceinline__ int sort_key(const SortArgs &a, long at, long n) {
     return at < n ? a.first ? a.tok(at) : a.key_in[at] : -1;
 }
-__device__ __forceinline__ void clear_present(const SortArgs &a, int threads) {
-    if (a.first && a.present)
-        for (long v = (long)blockIdx.x * threads + threadIdx.x; v < a.V; v += (long)gridDim.x * threads) a.present[v] = 0;
+__device__ __forceinline__ void clear_present(const SortArgs &a) {      // (its length is a multiple of 16)
+    uint4 *const p = reinterpret_cast<uint4 *>(a.present);
+    if (a.first && p)
+        for (long v = (long)blockIdx.x * kSortThreads + threadIdx.x; v < (a.V + 15) / 16; v += (long)gridDim.x * kSortThreads)
+            p[v] = make_uint4(0, 0, 0, 0);
 }
 
-// Adds a wave's digits to counts.  Text is made of few tokens: the digit of the first lane that has one is
-// counted by all lanes at once, the others by an atomic each.
-__device__ __forceinline__ void count_digits(int *h, bool has, int digit) {
-    const unsigned long long any = __ballot(has);
-    if (!any) return;
-    const int common = __builtin_amdgcn_readlane(digit, __ffsll(any) - 1);
-    const unsigned long long same = __ballot(has && digit == common);
-    if (has && digit != common) atomicAdd(&h[digit], 1);
-    if ((threadIdx.x & 63) == 0) atomicAdd(&h[common], __popcll(same));
+// Rank of each of a lane's items among its wave's with the same digit; `mine` (the wave's counts by digit, zero
+// before) holds how many there are of each afterwards.  Items without a token (key < 0) take no part.
+template <int R>
+__device__ __forceinline__ void rank_items(const int (&key)[R], int shift, int bits, int *mine, int (&rank)[R]) {
+    const int lane = threadIdx.x & 63, mask = (1 << bits) - 1;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const bool has = key[i] >= 0;
+        const int digit = (key[i] >> shift) & mask;
+        unsigned long long same = __ballot(has);
+        for (int b = 0; b < bits; ++b) {
+            const unsigned long long set = __ballot((digit >> b) & 1);
+            same &= (digit >> b) & 1 ? set : ~set;
+        }
+        const int lower = __popcll(same & ((1ull << lane) - 1));
+        int before = 0;
+        if (has) before = mine[digit];
+        __builtin_amdgcn_wave_barrier();
+        if (has && lower == 0) mine[digit] = before + __popcll(same);
+        __builtin_amdgcn_wave_barrier();
+        rank[i] = before + lower;
+    }
 }
 
-__global__ __launch_bounds__(kThreads) void sort_count_kernel(SortArgs a) {
+// Exclusive sum over a block's threads.
+__device__ __forceinline__ int sum_before(int mine, int *part, int *all) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    int upto = mine;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int v = __shfl_up(upto, m);
+        if (lane >= m) upto += v;
+    }
+    if (lane == 63) part[w] = upto;
+    __syncthreads();
+    int before = upto - mine;
+    *all = 0;
+#pragma unroll
+    for (int q = 0; q < kSortWaves; ++q) {
+        before += q < w ? part[q] : 0;
+        *all += part[q];
+    }
+    return before;
+}
+
+// counts [waves][digits] -> places, given where each digit begins
+__device__ __forceinline__ void places_of(int *counts, int digit, int at) {
+#pragma unroll
+    for (int q = 0; q < kSortWaves; ++q) {
+        const int c = counts[q * kDigits + digit];
+        counts[q * kDigits + digit] = at;
+        at += c;
+    }
+}
+
+template <int R>
+__global__ __launch_bounds__(kSortThreads) void sort_block_kernel(SortArgs a) {
+    __shared__ int keys[R * kSortThreads];
+    __shared__ unsigned short rows[R * kSortThreads];
+    __shared__ int counts[kSortWaves * kDigits];
+    __shared__ int part[kSortWaves];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, begin = w * R * 64 + lane;
+    int key[R], row[R], rank[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        row[i] = begin + i * 64;
+        key[i] = sort_key(a, row[i], a.N);
+    }
+    clear_present(a);
+    int n = 0;
+    for (int p = 0; p < a.passes; ++p) {
+        const int shift = p * a.bits;
+        for (int i = tid; i < kSortWaves * kDigits; i += kSortThreads) counts[i] = 0;
+        __syncthreads();
+        rank_items<R>(key, shift, a.bits, counts + w * kDigits, rank);
+        __syncthreads();
+        int sum = 0;
+        if (tid < kDigits)
+#pragma unroll
+            for (int q = 0; q < kSortWaves; ++q) sum += counts[q * kDigits + tid];
+        const int at = sum_before(sum, part, &n);
+        if (tid < kDigits) places_of(counts, tid, at);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (key[i] >= 0) {
+                const int to = counts[w * kDigits + ((key[i] >> shift) & ((1 << a.bits) - 1))] + rank[i];
+                keys[to] = key[i];
+                rows[to] = (unsigned short)row[i];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const bool has = begin + i * 64 < n;
+            key[i] = has ? keys[begin + i * 64] : -1;
+            row[i] = has ? rows[begin + i * 64] : 0;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+        if (key[i] >= 0) {
+            a.key_out[begin + i * 64] = key[i];
+            a.idx_out[begin + i * 64] = row[i];
+            if (a.present) a.present[key[i]] = 1;
+        }
+    if (tid == 0) *a.count = n;
+}
+
+// Text is made of few tokens: the digit of the first lane that has one is counted by all lanes at once, the
+// others by an atomic each.
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortArgs a) {
     __shared__ int h[kDigits];
     const int nd = 1 << a.bits, tid = threadIdx.x;
-    for (int d = tid; d < nd; d += kThreads) h[d] = 0;
-    clear_present(a, kThreads);
+    if (tid < nd) h[tid] = 0;
+    clear_present(a);
     __syncthreads();
     const long begin = (long)blockIdx.x * kItems, n = a.first ? a.N : (long)*a.count;
-#pragma unroll
-    for (int i = 0; i < kItems / kThreads; ++i) {
-        const int key = sort_key(a, begin + i * kThreads + tid, n);
-        count_digits(h, key >= 0, (key >> a.shift) & (nd - 1));
+    const int key = sort_key(a, begin + tid, n), digit = (key >> a.shift) & (nd - 1);
+    if (const unsigned long long any = __ballot(key >= 0)) {
+        const int common = __builtin_amdgcn_readlane(digit, __ffsll(any) - 1);
+        const unsigned long long same = __ballot(key >= 0 && digit == common);
+        if (key >= 0 && digit != common) atomicAdd(&h[digit], 1);
+        if ((tid & 63) == 0) atomicAdd(&h[common], __popcll(same));
     }
     __syncthreads();
-    for (int d = tid; d < nd; d += kThreads) a.hist[(size_t)blockIdx.x * nd + d] = h[d];
+    if (tid < nd) a.hist[(size_t)blockIdx.x * nd + tid] = h[tid];
 }
 
 // Counts to places, by digit: 64 digits a block, 16 threads walk the blocks of one.
-__global__ __launch_bounds__(1024) void sort_columns_kernel(SortArgs a) {
+__global__ __launch_bounds__(kSortThreads) void sort_columns_kernel(SortArgs a) {
     __shared__ int sums[16][64];
     const int nd = 1 << a.bits, lane = threadIdx.x & 63, w = threadIdx.x >> 6, d = blockIdx.x * 64 + lane;
     const int each = (a.blocks + 15) / 16, from = w * each, to = from + each < a.blocks ? from + each : a.blocks;
@@ -210,77 +318,41 @@ __global__ __launch_bounds__(1024) void sort_columns_kernel(SortArgs a) {
     }
 }
 
-// One item a thread.  A lane's rank is the number of lower lanes with its digit; waves follow each
-// other by their counts.
-constexpr int kPlaceWaves = kItems / 64;
-__global__ __launch_bounds__(kItems) void sort_place_kernel(SortArgs a) {
-    __shared__ int base[kDigits];
-    __shared__ int mine[kPlaceWaves * kDigits];              // [waves][digits]; before that, counts of all and of earlier items
-    __shared__ int part[kPlaceWaves];
-    const int nd = 1 << a.bits, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a) {
+    __shared__ int counts[kSortWaves * kDigits];
+    __shared__ int part[kSortWaves];
+    const int nd = 1 << a.bits, tid = threadIdx.x, w = tid >> 6;
     const long n = a.first ? a.N : (long)*a.count;
-    const long begin = (long)blockIdx.x * kItems, at = begin + tid;
-    const int key = sort_key(a, at, n), digit = (key >> a.shift) & (nd - 1);
-    const int idx = a.first || at >= n ? (int)at : a.idx_in[at];
-    const bool has = key >= 0;
-    int sum = 0, before = 0;
-    if (!a.hist) {
-        clear_present(a, kItems);
-        int *all = mine, *early = mine + kDigits;
-        for (int d = tid; d < nd; d += kItems) all[d] = early[d] = 0;
-        __syncthreads();
-        constexpr int U = 8;                                 // blocks of items read at a time
-        for (long b = 0; b * kItems < n; b += U) {
-            int k[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) k[u] = sort_key(a, (b + u) * kItems + tid, n);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                count_digits(b + u < (long)blockIdx.x ? early : all, k[u] >= 0, (k[u] >> a.shift) & (nd - 1));
-        }
-        __syncthreads();
-        if (tid < nd) { before = early[tid]; sum = all[tid] + before; }
-        __syncthreads();
-    } else if (tid < nd) {
-        sum = a.totals[tid];
-        before = a.hist[(size_t)blockIdx.x * nd + tid];
-    }
-    // the digits before a digit
-    int upto = sum;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const int v = __shfl_up(upto, m);
-        if (lane >= m) upto += v;
-    }
-    if (lane == 63) part[w] = upto;
-    for (int i = tid; i < kPlaceWaves * nd; i += kItems) mine[i] = 0;
-    __syncthreads();
-    int offset = upto - sum, all = 0;
-#pragma unroll
-    for (int q = 0; q < kPlaceWaves; ++q) {
-        offset += q < w ? part[q] : 0;
-        all += part[q];
-    }
-    if (tid < nd) base[tid] = offset + before;
-    if (a.first && blockIdx.x == 0 && tid == 0) *a.count = all;
-    unsigned long long same = __ballot(has);
-    for (int b = 0; b < a.bits; ++b) {
-        const unsigned long long set = __ballot((digit >> b) & 1);
-        same &= (digit >> b) & 1 ? set : ~set;
-    }
-    const int rank = __popcll(same & ((1ull << lane) - 1));
-    if (has && rank == 0) mine[w * nd + digit] = __popcll(same);
-    __syncthreads();
+    const long item = (long)blockIdx.x * kItems + tid;
+    const int key[1] = {sort_key(a, item, n)}, row = a.first || item >= n ? (int)item : a.idx_in[item];
+    int rank[1];
+    for (int i = tid; i < kSortWaves * kDigits; i += kSortThreads) counts[i] = 0;
+    int sum = 0, before = 0;             // of digit tid: in all blocks, in the blocks before this one
     if (tid < nd) {
-        int to = base[tid];
-        for (int q = 0; q < kPlaceWaves; ++q) { const int c = mine[q * nd + tid]; mine[q * nd + tid] = to; to += c; }
+        if (a.placed) {
+            sum = a.totals[tid];
+            before = a.hist[(size_t)blockIdx.x * nd + tid];
+        } else {
+#pragma unroll 16
+            for (int b = 0; b < a.blocks; ++b) {
+                const int h = a.hist[(size_t)b * nd + tid];
+                sum += h;
+                before += b < (int)blockIdx.x ? h : 0;
+            }
+        }
     }
     __syncthreads();
-    if (has) {
-        const int place = mine[w * nd + digit] + rank;
-        a.key_out[place] = key;
-        a.idx_out[place] = idx;
-        if (a.last && a.present) a.present[key] = 1;
+    rank_items<1>(key, a.shift, a.bits, counts + w * kDigits, rank);
+    int all;
+    const int at = sum_before(sum, part, &all) + before;      // (its barrier: the waves' counts are there)
+    if (a.first && blockIdx.x == 0 && tid == 0) *a.count = all;
+    if (tid < nd) places_of(counts, tid, at);
+    __syncthreads();
+    if (key[0] >= 0) {
+        const int to = counts[w * kDigits + ((key[0] >> a.shift) & (nd - 1))] + rank[0];
+        a.key_out[to] = key[0];
+        a.idx_out[to] = row;
+        if (a.last && a.present) a.present[key[0]] = 1;
     }
 }
 
@@ -446,17 +518,17 @@ GradPlan grad_plan(int dtype, long N, int D, int V, int T) {
     if (p.lanes < 8) p.lanes = 8;
     p.slices = (cpr + p.lanes - 1) / p.lanes;
     // chunks short enough for 128k threads, long enough that the parts they leave are few
-    const long c = N * (long)cpr / 131072;
-    p.C = (int)(c < 16 ? 16 : c > kMostChunk ? kMostChunk : c);
+    const long c = N * (long)cpr / 131072, least = N <= 8192 ? 4 : 16;
+    p.C = (int)(c < least ? least : c > kMostChunk ? kMostChunk : c);
     p.chunks = (N + p.C - 1) / p.C;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at = up(at + bytes, 256); return o; };
     p.rows = take(T ? (size_t)N * D * type_bytes(dtype) : 0);
     for (int i = 0; i < 2; ++i) { p.key[i] = take((size_t)N * 4); p.idx[i] = take((size_t)N * 4); }
-    p.hist = take(N > kShort ? (size_t)p.sort.blocks * (4u << p.sort.bits) : 0);
+    p.hist = take(p.sort.one ? 0 : (size_t)p.sort.blocks * (4u << p.sort.bits));
     p.totals = take(4u << p.sort.bits);
     p.count = take(4);
-    p.present = take(V);
+    p.present = take((size_t)V + 15);
     p.head = take((size_t)p.chunks * D * 4);
     p.tail = take((size_t)p.chunks * D * 4);
     p.total = at;
@@ -496,21 +568,28 @@ hipError_t accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, 
     SortArgs so{};
     so.tok = tok;
     so.count = reinterpret_cast<int *>(ws + p.count);
+    so.hist = reinterpret_cast<int *>(ws + p.hist); so.totals = reinterpret_cast<int *>(ws + p.totals);
     so.present = accumulate ? nullptr : reinterpret_cast<unsigned char *>(ws + p.present);
-    so.N = N; so.V = V; so.bits = p.sort.bits; so.blocks = p.sort.blocks;
-    if (N > kShort) { so.hist = reinterpret_cast<int *>(ws + p.hist); so.totals = reinterpret_cast<int *>(ws + p.totals); }
-    for (int i = 0; i < p.sort.passes; ++i) {
-        so.first = i == 0; so.last = i + 1 == p.sort.passes;
-        so.shift = i * p.sort.bits;
-        so.key_in = reinterpret_cast<int *>(ws + p.key[(i + 1) & 1]);
-        so.idx_in = reinterpret_cast<int *>(ws + p.idx[(i + 1) & 1]);
-        so.key_out = reinterpret_cast<int *>(ws + p.key[i & 1]);
-        so.idx_out = reinterpret_cast<int *>(ws + p.idx[i & 1]);
-        if (so.hist) {
-            hipLaunchKernelGGL(sort_count_kernel, dim3(so.blocks), dim3(kThreads), 0, s, so);
-            hipLaunchKernelGGL(sort_columns_kernel, dim3(((1 << so.bits) + 63) / 64), dim3(1024), 0, s, so);
+    so.N = N; so.V = V; so.bits = p.sort.bits; so.passes = p.sort.passes; so.blocks = p.sort.blocks;
+    so.placed = p.sort.blocks > kInline;
+    so.key_out = reinterpret_cast<int *>(ws + p.key[0]);
+    so.idx_out = reinterpret_cast<int *>(ws + p.idx[0]);
+    if (p.sort.one) {
+        so.first = 1;
+        if (N <= 1024) hipLaunchKernelGGL(sort_block_kernel<1>, dim3(1), dim3(kSortThreads), 0, s, so);
+        else hipLaunchKernelGGL(sort_block_kernel<4>, dim3(1), dim3(kSortThreads), 0, s, so);
+    } else {
+        for (int i = 0; i < p.sort.passes; ++i) {
+            so.first = i == 0; so.last = i + 1 == p.sort.passes;
+            so.shift = i * p.sort.bits;
+            so.key_in = reinterpret_cast<int *>(ws + p.key[(i + 1) & 1]);
+            so.idx_in = reinterpret_cast<int *>(ws + p.idx[(i + 1) & 1]);
+            so.key_out = reinterpret_cast<int *>(ws + p.key[i & 1]);
+            so.idx_out = reinterpret_cast<int *>(ws + p.idx[i & 1]);
+            hipLaunchKernelGGL(sort_count_kernel, dim3(so.blocks), dim3(kSortThreads), 0, s, so);
+            if (so.placed) hipLaunchKernelGGL(sort_columns_kernel, dim3(((1 << so.bits) + 63) / 64), dim3(kSortThreads), 0, s, so);
+            hipLaunchKernelGGL(sort_place_kernel, dim3(so.blocks), dim3(kSortThreads), 0, s, so);
         }
-        hipLaunchKernelGGL(sort_place_kernel, dim3(so.blocks), dim3(kItems), 0, s, so);
     }
     SumArgs<T> a{};
     a.gy = rows;

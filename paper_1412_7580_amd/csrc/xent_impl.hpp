@@ -31,9 +31,9 @@ constexpr int kThreads = 256;
 // ---------------------------------------------------------------------------------- rows with a target
 // The rows that have a target, packed in their order: blocks of 1024 rows place theirs behind those of the
 // blocks before them.  Up to kScanInline blocks each counts all rows itself; beyond that the blocks' counts
-// come from a launch of their own.  (One block for all rows: 38 us for 15488 of them, beside 10 for two
-// launches and 7 for one.)
-constexpr int kScanRows = 1024, kScanInline = 16;
+// come from a launch of their own.  (15488 rows: 38 us by one block, 22 by blocks that count all, 10 by two
+// launches.)
+constexpr int kScanRows = 1024, kScanInline = 4;
 
 struct ScanArgs {
     Tokens tok;
@@ -94,16 +94,13 @@ __global__ __launch_bounds__(kThreads) void xent_place_kernel(ScanArgs a) {
     int b4 = 0, sum = 0;
     float top = r.top;
     if (a.blocks <= kScanInline)
-        for (int b = 0; b < a.blocks; ++b) {
-            if (b == (int)blockIdx.x) { sum += r.mine; continue; }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const long n = (long)b * kScanRows + e * kThreads + tid;
-                const bool has = n < a.N && a.tok(n) >= 0;
-                b4 += has && b < (int)blockIdx.x;
-                sum += has;
-                if (has && a.gloss) top = fmaxf(top, fabsf(a.gloss[n]));
-            }
+        for (int i = 0; i < kScanInline * 4; ++i) {
+            const long n = (long)i * kThreads + tid;
+            const bool has = n < a.N && a.tok(n) >= 0;
+            b4 += has && n < n0;
+            sum += has;
+            if (has && a.gloss) top = fmaxf(top, fabsf(a.gloss[n]));
         }
     else
         for (int b = tid; b < a.blocks; b += kThreads) {
