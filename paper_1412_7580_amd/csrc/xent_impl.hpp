@@ -271,33 +271,60 @@ struct RowsOutArgs {
     int bm, tiles_n, places, most, D, T_;
 };
 
-template <class S>
-__device__ __forceinline__ void sum8(const RowsOutArgs<S> &a, int c, int d, float alpha, float (&f)[8]) {
+// The sum of parts from, from + 1, ... below to, eight of them asked for at a time.
+__device__ __forceinline__ void sum_parts(const float *p, size_t stride, int from, int to, int n, float (&f)[8]) {
+    constexpr int U = 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = 0.f;
-    if (c < 0) return;
-    const int tiles_m = (*a.count + a.bm - 1) / a.bm, splits = rows_splits((long)tiles_m * a.tiles_n, a.places, a.most);
-    for (int s = 0; s < splits; ++s) {
-        float v[8];
-        load8(a.partial + ((size_t)s * tiles_m * a.bm + c) * a.ld + d, a.D - d, v);
+    for (int s = from; s < to; s += U) {
+        float v[U][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] += v[i];
+        for (int u = 0; u < U; ++u)
+            if (s + u < to) load8(p + (s + u) * stride, n, v[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (s + u < to)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] += v[u][i];
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] *= alpha;
 }
 
+struct RowParts { int splits; size_t stride; };
 template <class S>
+__device__ __forceinline__ RowParts parts_of(const RowsOutArgs<S> &a) {
+    const int tiles_m = (*a.count + a.bm - 1) / a.bm;
+    return RowParts{rows_splits((long)tiles_m * a.tiles_n, a.places, a.most), (size_t)tiles_m * a.bm * a.ld};
+}
+
+// G threads share a piece of eight columns where there are many parts and few rows.
+template <class S, int G>
 __global__ __launch_bounds__(kThreads) void xent_rows_out_kernel(RowsOutArgs<S> a) {
-    const int cpr = (a.D + 7) / 8;
+    __shared__ float sums[G > 1 ? kThreads : 1][9];
+    constexpr int B = kThreads / G;
+    const int cpr = (a.D + 7) / 8, g = threadIdx.x / B;
     const size_t total = (size_t)a.N * cpr;
     const float alpha = *a.alpha;
-    for (size_t c = (size_t)blockIdx.x * kThreads + threadIdx.x; c < total; c += (size_t)gridDim.x * kThreads) {
+    const RowParts parts = parts_of(a);
+    const int each = (parts.splits + G - 1) / G, from = g * each, to = from + each < parts.splits ? from + each : parts.splits;
+    for (size_t c0 = (size_t)blockIdx.x * B; c0 < total; c0 += (size_t)gridDim.x * B) {
+        const size_t c = c0 + threadIdx.x % B;
         const long n = (long)(c / cpr);
-        const int d = (int)(c - (size_t)n * cpr) * 8;
-        float f[8];
-        sum8(a, a.pos[n], d, alpha, f);
-        store8(a.gx + (size_t)n * a.D + d, a.D - d, f);
+        const int d = (int)(c - (size_t)n * cpr) * 8, at = c < total ? a.pos[n] : -1;
+        float f[8] = {};
+        if (at >= 0) sum_parts(a.partial + (size_t)at * a.ld + d, parts.stride, from, to, a.D - d, f);
+        if constexpr (G > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sums[threadIdx.x][i] = f[i];
+            __syncthreads();
+            if (g > 0) continue;
+            for (int q = 1; q * each < parts.splits; ++q)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] += sums[q * B + threadIdx.x][i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] *= alpha;
+        if (c < total) store8(a.gx + (size_t)n * a.D + d, a.D - d, f);
     }
 }
 
@@ -308,12 +335,16 @@ __global__ __launch_bounds__(kThreads) void xent_planes_out_kernel(RowsOutArgs<S
     const unsigned per = tiles_d * tiles_t, s = blockIdx.x / per, rest = blockIdx.x - s * per;
     const int t0 = (int)(rest % tiles_t) * 64, d0 = (int)(rest / tiles_t) * 64;
     const float alpha = *a.alpha;
+    const RowParts parts = parts_of(a);
     for (int c = threadIdx.x; c < 64 * 8; c += kThreads) {
         const int q = c >> 3, dd = (c & 7) * 8;
         float f[8] = {};
-        if (t0 + q < a.T_ && d0 + dd < a.D) sum8(a, a.pos[(long)s * a.T_ + t0 + q], d0 + dd, alpha, f);
+        if (t0 + q < a.T_ && d0 + dd < a.D) {
+            const int at = a.pos[(long)s * a.T_ + t0 + q];
+            if (at >= 0) sum_parts(a.partial + (size_t)at * a.ld + d0 + dd, parts.stride, 0, parts.splits, a.D - d0 - dd, f);
+        }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) tile[dd + i][q] = f[i];
+        for (int i = 0; i < 8; ++i) tile[dd + i][q] = f[i] * alpha;
     }
     __syncthreads();
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -339,13 +370,8 @@ __global__ __launch_bounds__(kThreads) void xent_classes_out_kernel(ClassesOutAr
     for (size_t c = (size_t)blockIdx.x * kThreads + threadIdx.x; c < total; c += (size_t)gridDim.x * kThreads) {
         const long m = (long)(c / cpr);
         const int d = (int)(c - (size_t)m * cpr) * 8;
-        float f[8] = {};
-        for (int s = 0; s < a.splits; ++s) {
-            float v[8];
-            load8(a.partial + ((size_t)s * a.M + m) * a.ld + d, a.D - d, v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] += v[i];
-        }
+        float f[8];
+        sum_parts(a.partial + (size_t)m * a.ld + d, (size_t)a.M * a.ld, 0, a.splits, a.D - d, f);
         float old[8] = {};
         if (a.add) load8(a.gw + (size_t)m * a.D + d, a.D - d, old);
 #pragma unroll
@@ -590,12 +616,14 @@ struct XentPlan {
     size_t row_of, pos, target, count, counts, tops, lse, coef, hit, part, x, w, G, gx, gw, total;
 };
 
-// Few rows: as many tiles of 16 of them as a block's LDS holds, four at most.  More groups of rows than
-// one read the weights again, which the other path's packing and narrow tiles cost too; in fp32 that path
-// also cuts and multiplies every weight six times.
+// Few rows: as many tiles of 16 of them as a block's LDS holds, four at most.  More groups of rows read the
+// weights again; the other path reads them once, but packs the rows, wastes most of a 128-row tile and copies
+// weights whose rows are no whole 16 bytes, or cuts fp32 ones into terms.  32000 classes of 1024 features, us by
+// this path and the other: bf16 18 and 32 (1 row), 28 and 33 (128, two groups), 39 and 37 (192); fp32 35 and 156
+// (1), 152 and 170 (192, six groups), 194 and 171 (256).  20001 classes of 333, bf16: 36 and 38 (256, four groups).
 inline void thin_plan(XentPlan &p, int dtype, long N, int D, int V) {
     const int s = (int)type_bytes(dtype), ks = dtype == kF32 ? 16 : 32;
-    const long row = (ceil_to(D, ks) + 16 / s) * s, groups_most = dtype == kF32 ? 4 : 2;
+    const long row = (ceil_to(D, ks) + 16 / s) * s, groups_most = dtype == kF32 ? 6 : D % 8 ? 4 : 2;
     int t = N <= 16 ? 1 : N <= 32 ? 2 : 4;
     while (t > 1 && t * 16 * row > kThinLds) t /= 2;
     if (t * 16 * row > kThinLds || N > groups_most * t * 16) return;
@@ -814,7 +842,9 @@ struct Xent {
                 if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
                 hipLaunchKernelGGL(xent_planes_out_kernel<S>, dim3((unsigned)blocks), dim3(kThreads), 0, s, o);
             } else {
-                hipLaunchKernelGGL(xent_rows_out_kernel<S>, dim3(blocks_for((size_t)c.N * ((c.D + 7) / 8))), dim3(kThreads), 0, s, o);
+                const size_t pieces = (size_t)c.N * ((c.D + 7) / 8);
+                if (p.rows.splits > 8) hipLaunchKernelGGL((xent_rows_out_kernel<S, 8>), dim3(blocks_for(pieces * 8)), dim3(kThreads), 0, s, o);
+                else hipLaunchKernelGGL((xent_rows_out_kernel<S, 1>), dim3(blocks_for(pieces)), dim3(kThreads), 0, s, o);
             }
         }
         return hipGetLastError();
