@@ -590,10 +590,10 @@ inline long places(const Shape &s) { return s.bm == 256 ? kBigPlaces : kSmallPla
 // Where the reduction may be split, it is, until there is a block for every place; such products take
 // tiles 192 columns wide where that covers the columns with less (384 columns: 97 -> 70 us for 15488 rows
 // and 1000 classes in fp32).
-inline Shape shape_of(long M, long N, long K, bool split) {
-    const long steps = (K + kStep - 1) / kStep;
+inline Shape shape_of(long M, long N, long K, int terms, bool split) {
+    const long steps = (K + kStep - 1) / kStep, parts = steps * (terms == 3 ? 6 : 1) / 6;      // of six products at least
     Shape s{};
-    s.most = split ? (int)(steps / 8 < 1 ? 1 : steps / 8 > 64 ? 64 : steps / 8) : 1;
+    s.most = split ? (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts) : 1;
     const auto tiles = [](long n, long t) { return (n + t - 1) / t; };
     s.bm = 256;
     s.bn = split && tiles(N, 192) * 192 < tiles(N, 256) * 256 ? 192 : 256;
@@ -662,7 +662,7 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
     p.x = take((size_t)p.Np * p.terms * p.Dp * 2);
     p.w = take(p.pack_w ? (size_t)V * p.terms * p.Dp * 2 : 0);
     if (!backward) {
-        p.score = shape_of(N, V, D, false);
+        p.score = shape_of(N, V, D, p.terms, false);
         p.hit = take((size_t)N * 4);
         p.part = take((size_t)p.score.tiles_n * p.Np * 8);
     } else {
@@ -675,9 +675,9 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
         p.piece = (int)ceil_to(((long)V + p.pieces - 1) / p.pieces, 256);
         p.pieces = (int)(((long)V + p.piece - 1) / p.piece);
         const long widest = p.piece < V ? p.piece : V;
-        p.score = shape_of(N, widest, D, false);
-        p.rows = shape_of(N, D, widest, true);
-        p.classes = shape_of(widest, D, N, true);
+        p.score = shape_of(N, widest, D, p.terms, false);
+        p.rows = shape_of(N, D, widest, p.terms, true);
+        p.classes = shape_of(widest, D, N, p.terms, true);
         p.G = take((size_t)p.Np * p.terms * ceil_to(widest, 64) * 2);
         // the rows product splits by the tiles of rows that have a target: the fewer, the more parts, but never more
         // tiles in all than places, or than one part of all rows
