@@ -535,12 +535,20 @@ GradPlan grad_plan(int dtype, long N, int D, int V, int T) {
     return p;
 }
 
+long sum_blocks(const GradPlan &p) {
+    const long groups = kThreads / p.lanes;
+    return (p.chunks * p.slices + groups - 1) / groups;
+}
+int zero_rows(int D) {
+    const int rows = 1024 / ((D + 7) / 8);
+    return rows < 1 ? 1 : rows > 64 ? 64 : rows;
+}
+
 template <class T>
 hipError_t fprop(const void *table, Tokens tok, void *y, long N, int D, int Tn, float scale, hipStream_t s) {
     if (Tn) {
         PlaneArgs<T> a{static_cast<const T *>(table), tok, static_cast<T *>(y), D, Tn, (Tn + 63) / 64, (D + 63) / 64, scale};
         const long blocks = N / Tn * a.tiles_t * a.tiles_d;
-        if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
         hipLaunchKernelGGL(embedding_planes_kernel<T>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
         return hipGetLastError();
     }
@@ -561,7 +569,6 @@ hipError_t accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, 
     if (Tn) {
         TurnArgs<T> t{rows, tok, reinterpret_cast<T *>(ws + p.rows), D, Tn, (Tn + 63) / 64, (D + 63) / 64};
         const long blocks = N / Tn * t.tiles_t * t.tiles_d;
-        if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
         hipLaunchKernelGGL(planes_to_rows_kernel<T>, dim3((unsigned)blocks), dim3(kThreads), 0, s, t);
         rows = t.rows;
     }
@@ -599,12 +606,9 @@ hipError_t accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, 
     a.tail = reinterpret_cast<float *>(ws + p.tail);
     a.chunks = p.chunks; a.D = D; a.V = V; a.C = p.C; a.lanes = p.lanes; a.slices = p.slices;
     a.scale = scale; a.accumulate = accumulate;
-    const long groups = kThreads / p.lanes;
-    a.sum_blocks = (p.chunks * p.slices + groups - 1) / groups;
-    const int cpr = (D + 7) / 8;
-    a.zero_rows = 1024 / cpr < 1 ? 1 : 1024 / cpr > 64 ? 64 : 1024 / cpr;
+    a.sum_blocks = sum_blocks(p);
+    a.zero_rows = zero_rows(D);
     const long zero_blocks = accumulate ? 0 : ((long)V + a.zero_rows - 1) / a.zero_rows;
-    if (a.sum_blocks + zero_blocks > 0x7fffffffL) return hipErrorInvalidValue;
     hipLaunchKernelGGL(embedding_sum_kernel<T>, dim3((unsigned)(a.sum_blocks + zero_blocks)), dim3(kThreads), 0, s, a);
     if (p.chunks > 1) hipLaunchKernelGGL(embedding_join_kernel<T>, dim3((unsigned)p.chunks), dim3(kThreads), 0, s, a);
     return hipGetLastError();
@@ -613,6 +617,14 @@ hipError_t accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, 
 }  // namespace
 
 size_t embedding_accgrad_bytes(int dtype, long N, int D, int V, int T) { return N ? grad_plan(dtype, N, D, V, T).total : 0; }
+
+bool embedding_fits(bool accgrad, long N, int D, int V, int T) {
+    if (N == 0) return true;
+    if (T && (double)N / T * ((T + 63) / 64) * ((D + 63) / 64) > 0x7fffffff) return false;
+    if (!accgrad) return true;
+    const GradPlan p = grad_plan(kF32, N, D, V, T);
+    return p.chunks <= 0x7fffffff && (double)sum_blocks(p) + ((double)V / zero_rows(D) + 1) <= 0x7fffffff;
+}
 
 hipError_t launch_embedding_fprop(int dtype, const void *table, Tokens tok, void *y, long N, int D, int T, float scale, hipStream_t s) {
     if (N == 0) return hipSuccess;

@@ -163,7 +163,6 @@ hipError_t launch_grad_norm(int count, const void *const *grads, const long *siz
     NormArgs a;
     a.piece = piece_length(count, sizes);
     const long pieces = pieces_of(count, sizes, a.piece);
-    if (pieces > 0x7fffffffL) return hipErrorInvalidValue;
     a.sums = static_cast<double *>(ws);
     a.norm = norm;
     a.max_norm = max_norm;

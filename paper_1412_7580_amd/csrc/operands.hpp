@@ -75,6 +75,7 @@ struct RowsOf {
 
 // ---- embedding.hip
 size_t embedding_accgrad_bytes(int dtype, long N, int D, int V, int T);
+bool embedding_fits(bool accgrad, long N, int D, int V, int T);              // whether one launch takes each of its grids
 hipError_t launch_embedding_fprop(int dtype, const void *table, Tokens tok, void *y, long N, int D, int T, float scale, hipStream_t s);
 hipError_t launch_embedding_accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, int D, int T, float scale,
                                     bool accumulate, void *ws, hipStream_t s);
@@ -98,7 +99,9 @@ struct XentCall {
     float scale;
     bool mean, accumulate;
 };
-size_t xent_bytes(bool backward, int dtype, long N, int D, int V);
+// aligned: the weights start at a multiple of 16 bytes (others are copied).
+size_t xent_bytes(bool backward, int dtype, long N, int D, int V, bool aligned);
+bool xent_fits(bool backward, int dtype, long N, int D, int V, int T);      // whether one launch takes each of its grids
 hipError_t xent_fprop_f32(const XentCall &c, void *ws, hipStream_t s);
 hipError_t xent_fprop_bf16(const XentCall &c, void *ws, hipStream_t s);
 hipError_t xent_fprop_f16(const XentCall &c, void *ws, hipStream_t s);

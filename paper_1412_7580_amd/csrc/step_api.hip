@@ -27,6 +27,7 @@ struct OnDevice {
 };
 
 constexpr long kMost = 1L << 30;      // rows, features, classes: positions are held in 32 bits
+constexpr int kMostFeatures = 1 << 20;    // of the cross entropy: a tile's byte offsets are
 
 int check_sizes(int dtype, int token_bits, long N, int D, int V, int T) {
     if (dtype < 0 || dtype > 2 || (token_bits != 32 && token_bits != 64)) return FFTCONV_INVALID_ARG;
@@ -48,11 +49,7 @@ int workspace(fftconv_ctx *c, size_t need, void **ws, size_t bytes) {
     return get_workspace(c, need, ws, 0);
 }
 
-int done(fftconv_ctx *c, hipError_t e) {
-    if (e == hipSuccess) return FFTCONV_OK;
-    if (e == hipErrorInvalidValue) return FFTCONV_UNSUPPORTED;    // a grid beyond what one launch takes
-    return hip_fail(c, e);
-}
+int done(fftconv_ctx *c, hipError_t e) { return e == hipSuccess ? FFTCONV_OK : hip_fail(c, e); }
 
 int check_list(int count, const void *const *grads, const long *sizes, const int *dtypes) {
     if (count < 0 || (count > 0 && (!grads || !sizes || !dtypes))) return FFTCONV_INVALID_ARG;
@@ -106,6 +103,7 @@ int fftconv_embedding_fprop(fftconv_handle hd, int dtype, const void *table, con
     if (int rc = check_sizes(dtype, token_bits, N, D, V, T); rc != FFTCONV_OK) return rc;
     if (N == 0) return FFTCONV_OK;
     if (!table || !tokens || !y) return FFTCONV_INVALID_ARG;
+    if (!embedding_fits(false, N, D, V, T)) return FFTCONV_UNSUPPORTED;
     const OnDevice on(hd->device);
     if (on.error != hipSuccess) return hip_fail(hd, on.error);
     return done(hd, launch_embedding_fprop(dtype, table, Tokens{tokens, token_bits == 64, V}, y, N, D, T, scale, hd->stream));
@@ -121,6 +119,7 @@ int fftconv_embedding_accgrad(fftconv_handle hd, int dtype, const void *gy, cons
     if (!hd || !gtable) return FFTCONV_INVALID_ARG;
     if (int rc = check_sizes(dtype, token_bits, N, D, V, T); rc != FFTCONV_OK) return rc;
     if (N > 0 && (!gy || !tokens)) return FFTCONV_INVALID_ARG;
+    if (!embedding_fits(true, N, D, V, T)) return FFTCONV_UNSUPPORTED;
     const OnDevice on(hd->device);
     if (on.error != hipSuccess) return hip_fail(hd, on.error);
     if (N > 0)
@@ -130,8 +129,8 @@ int fftconv_embedding_accgrad(fftconv_handle hd, int dtype, const void *gy, cons
 }
 
 size_t fftconv_xent_workspace_bytes(int pass, int dtype, long N, int D, int V) {
-    if (check_sizes(dtype, 64, N, D, V, 0) != FFTCONV_OK || (pass != FFTCONV_FPROP && pass != FFTCONV_BPROP)) return 0;
-    return xent_bytes(pass == FFTCONV_BPROP, dtype, N, D, V);
+    if (check_sizes(dtype, 64, N, D, V, 0) != FFTCONV_OK || D > kMostFeatures || (pass != FFTCONV_FPROP && pass != FFTCONV_BPROP)) return 0;
+    return xent_bytes(pass == FFTCONV_BPROP, dtype, N, D, V, false);
 }
 
 int fftconv_xent_fprop(fftconv_handle hd, int dtype, const void *x, const void *wt, const void *targets, int token_bits,
@@ -140,9 +139,10 @@ int fftconv_xent_fprop(fftconv_handle hd, int dtype, const void *x, const void *
     if (int rc = check_sizes(dtype, token_bits, N, D, V, T); rc != FFTCONV_OK) return rc;
     if (N == 0) return FFTCONV_OK;
     if (!x || !wt || !targets || !loss || !lse) return FFTCONV_INVALID_ARG;
+    if (D > kMostFeatures || !xent_fits(false, dtype, N, D, V, T)) return FFTCONV_UNSUPPORTED;
     const OnDevice on(hd->device);
     if (on.error != hipSuccess) return hip_fail(hd, on.error);
-    if (int rc = workspace(hd, xent_bytes(false, dtype, N, D, V), &ws, ws_bytes); rc != FFTCONV_OK) return rc;
+    if (int rc = workspace(hd, xent_bytes(false, dtype, N, D, V, !ws && !(reinterpret_cast<size_t>(wt) & 15)), &ws, ws_bytes); rc != FFTCONV_OK) return rc;
     XentCall c{};
     c.dtype = dtype; c.x = x; c.wt = wt; c.tok = Tokens{targets, token_bits == 64, V};
     c.N = N; c.D = D; c.V = V; c.T = T; c.loss = loss; c.lse = lse;
@@ -156,13 +156,14 @@ int fftconv_xent_backward(fftconv_handle hd, int dtype, const void *x, const voi
     if (!hd) return FFTCONV_INVALID_ARG;
     if (int rc = check_sizes(dtype, token_bits, N, D, V, T); rc != FFTCONV_OK) return rc;
     if (N > 0 && (!x || !wt || !targets || !lse)) return FFTCONV_INVALID_ARG;
+    if (D > kMostFeatures || !xent_fits(true, dtype, N, D, V, T)) return FFTCONV_UNSUPPORTED;
     const OnDevice on(hd->device);
     if (on.error != hipSuccess) return hip_fail(hd, on.error);
     if (N == 0)      // no rows: the weights' gradient is zero, as the table's of no tokens is
         return gw ? done(hd, launch_embedding_accgrad(dtype, nullptr, Tokens{nullptr, 0, V}, gw, 0, D, 0, 0.f, accumulate != 0,
                                                       nullptr, hd->stream)) : FFTCONV_OK;
     if (!gx && !gw) return FFTCONV_OK;
-    if (int rc = workspace(hd, xent_bytes(true, dtype, N, D, V), &ws, ws_bytes); rc != FFTCONV_OK) return rc;
+    if (int rc = workspace(hd, xent_bytes(true, dtype, N, D, V, !ws && !(reinterpret_cast<size_t>(wt) & 15)), &ws, ws_bytes); rc != FFTCONV_OK) return rc;
     XentCall c{};
     c.dtype = dtype; c.x = x; c.wt = wt; c.tok = Tokens{targets, token_bits == 64, V};
     c.N = N; c.D = D; c.V = V; c.T = T; c.lse = const_cast<float *>(lse); c.gloss = gloss;

@@ -694,7 +694,6 @@ hipError_t product(GemmArgs &g, const Shape &sh, hipStream_t s) {
     g.tiles_m = sh.tiles_m; g.tiles_n = sh.tiles_n; g.splits = sh.splits;
     g.places = (int)places(sh); g.most = sh.most;
     const long tiles = (long)sh.tiles_m * sh.tiles_n * (END == kRows ? sh.most : sh.splits);
-    if (tiles > 0x7fffffffL) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(tiles < g.places ? tiles : g.places));
     const auto launch = [&](auto kernel, int threads, int lds) {
         if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(kernel), lds); e != hipSuccess) return e;
@@ -710,6 +709,15 @@ hipError_t product(GemmArgs &g, const Shape &sh, hipStream_t s) {
 inline unsigned blocks_for(size_t chunks) {
     const size_t b = (chunks + kThreads - 1) / kThreads;
     return (unsigned)(b < 1 ? 1 : b < 8192 ? b : 8192);
+}
+
+// Whether every launch of a call takes its grid.
+inline bool xent_launchable(const XentPlan &p, bool backward, long N, int D, int T) {
+    const auto fits = [](double blocks) { return blocks <= 0x7fffffff; };
+    if (p.thin_tiles) return true;                           // (a thousand rows at most)
+    if (T && (!fits((double)(p.Np / 64) * ((D + 63) / 64)) || !fits((double)N / T * ((T + 63) / 64) * ((D + 63) / 64)))) return false;
+    const auto product = [&](const Shape &s) { return fits((double)s.tiles_m * s.tiles_n * s.most); };
+    return backward ? product(p.score) && product(p.rows) && product(p.classes) : product(p.score);
 }
 
 // S: the operands' type in memory; T: the type the matrix cores take.
@@ -738,7 +746,6 @@ struct Xent {
         PackArgs<S, T, SPLIT> a{static_cast<const S *>(c.x), at<T>(p.x), at<int>(p.row_of), at<int>(p.count), p.Np, c.D, p.Dp, c.T};
         if (c.T) {
             const long blocks = p.Np / 64 * ((c.D + 63) / 64);
-            if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
             hipLaunchKernelGGL((xent_pack_planes_kernel<S, T, SPLIT>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
         } else {
             hipLaunchKernelGGL((xent_pack_kernel<S, T, SPLIT>), dim3(blocks_for((size_t)p.Np * p.Dp / 8)), dim3(kThreads), 0, s, a);
@@ -839,7 +846,6 @@ struct Xent {
                                    p.rows.bm, p.rows.tiles_n, (int)places(p.rows), p.rows.most, c.D, c.T};
             if (c.T) {
                 const long blocks = c.N / c.T * ((c.T + 63) / 64) * ((c.D + 63) / 64);
-                if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
                 hipLaunchKernelGGL(xent_planes_out_kernel<S>, dim3((unsigned)blocks), dim3(kThreads), 0, s, o);
             } else {
                 const size_t pieces = (size_t)c.N * ((c.D + 7) / 8);
