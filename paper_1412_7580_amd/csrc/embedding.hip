@@ -97,9 +97,16 @@ __global__ __launch_bounds__(kThreads) void planes_to_rows_kernel(TurnArgs<T> a)
     const unsigned s = blockIdx.x / per, rest = blockIdx.x - s * per;
     const int t0 = (int)(rest % a.tiles_t) * 64, d0 = (int)(rest / a.tiles_t) * 64;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    if (t0 + lane < a.T_)
-        for (int i = w; i < 64 && d0 + i < a.D; i += kWaves)
-            tile[i][lane] = to_float(a.gy[((size_t)s * a.D + d0 + i) * a.T_ + t0 + lane]);
+    if (t0 + lane < a.T_) {
+        T v[64 / kWaves];                                    // (all asked for before the first is stored)
+#pragma unroll
+        for (int i = 0; i < 64 / kWaves; ++i) {
+            const int d = d0 + i * kWaves + w;
+            v[i] = a.gy[((size_t)s * a.D + (d < a.D ? d : a.D - 1)) * a.T_ + t0 + lane];
+        }
+#pragma unroll
+        for (int i = 0; i < 64 / kWaves; ++i) tile[i * kWaves + w][lane] = to_float(v[i]);
+    }
     __syncthreads();
     for (int c = threadIdx.x; c < 64 * 8; c += kThreads) {
         const int r = c >> 3, dd = (c & 7) * 8, n = a.D - d0 - dd;

@@ -210,7 +210,14 @@ __global__ __launch_bounds__(kThreads) void xent_pack_planes_kernel(PackArgs<S, 
     if (r < count) {
         const RowsOf at{a.D, a.T_};
         const S *p = a.from + at.offset(a.row_of[r]);
-        for (int i = w; i < 64; i += 4) tile[i][lane] = d0 + i < a.D ? to_float(p[(size_t)(d0 + i) * a.T_]) : 0.f;
+        S v[16];                                             // (all asked for before the first is stored)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int d = d0 + i * 4 + w;
+            v[i] = p[(size_t)(d < a.D ? d : a.D - 1) * a.T_];
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) tile[i * 4 + w][lane] = d0 + i * 4 + w < a.D ? to_float(v[i]) : 0.f;
     } else {
         for (int i = w; i < 64; i += 4) tile[i][lane] = 0.f;
     }
