@@ -33,6 +33,7 @@ namespace fc {
 
 enum { kStats = 0, kGrad = 1, kRows = 2, kClasses = 3 };
 constexpr int kStep = 64;            // k per step
+constexpr float kLog2E = 1.44269504088896340736f;
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
@@ -99,6 +100,30 @@ __device__ __forceinline__ void lds_written_and_met() { asm volatile("s_waitcnt 
 template <int N>
 __device__ __forceinline__ void landed_and_met() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// What a lane and its partners 16 and 32 lanes on hold, by vector moves (the four sixteens' largest, or their sum).
+__device__ __forceinline__ float2 both16(float x) {
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const unsigned a = r[0], b = r[1];
+    return make_float2(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+__device__ __forceinline__ float2 both32(float x) {
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned a = r[0], b = r[1];
+    return make_float2(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+__device__ __forceinline__ float sixteens_max(float x) {
+    const float2 a = both16(x);
+    const float2 b = both32(fmaxf(a.x, a.y));
+    return fmaxf(b.x, b.y);
+}
+__device__ __forceinline__ float sixteens_sum(float x) {
+    const float2 a = both16(x);
+    const float2 b = both32(a.x + a.y);
+    return b.x + b.y;
 }
 
 template <class T> struct Mfma;
@@ -356,16 +381,14 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
                 float top = -INFINITY;
 #pragma unroll
                 for (int j = 0; j < FN; ++j) top = fmaxf(fmaxf(fmaxf(top, acc[i][j][0]), acc[i][j][1]), fmaxf(acc[i][j][2], acc[i][j][3]));
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
+                top = sixteens_max(top);
                 const float base = top == -INFINITY ? 0.f : top;  // (nothing but -inf: the sum is 0)
                 float sum = 0.f;
 #pragma unroll
                 for (int j = 0; j < FN; ++j)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) sum += __expf(acc[i][j][r] - base);
-                sum += __shfl_xor(sum, 16);
-                sum += __shfl_xor(sum, 32);
+                sum = sixteens_sum(sum);
                 if (lane < 16) both[wn * BM + lm] = make_float2(top, sum);
             }
             lds_written_and_met();
@@ -387,7 +410,7 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
                 const int lm = (wm * FM + i) * 16 + row;
                 const long m = m_at + lm;
                 const int rel = targets[lm] - a.n0 - (int)n_at - wn * FN * 16 - quad;
-                const float lse = lses[lm], coef = coefs[lm];
+                const float lse = lses[lm], coef = coefs[lm], lse2 = lse * kLog2E;
                 const bool hit = m < count && rel >= 0 && rel < FN * 16 && (rel & 12) == 0;
                 const bool any = __any(hit);
                 // Two column tiles at a time: lanes of odd sixteens trade theirs of the first tile for the second's of
@@ -399,8 +422,10 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         float g[4];
+                        // (for 16-bit operands one instruction less: off by the rounding of lse log2(e), as lse is by its own)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) g[r] = __expf(acc[i][j + h][r] - lse);
+                        for (int r = 0; r < 4; ++r)
+                            g[r] = SPLIT ? __expf(acc[i][j + h][r] - lse) : __builtin_amdgcn_exp2f(fmaf(acc[i][j + h][r], kLog2E, -lse2));
                         if (any)
 #pragma unroll
                             for (int r = 0; r < 4; ++r) g[r] -= hit && rel == (j + h) * 16 + r ? 1.f : 0.f;
