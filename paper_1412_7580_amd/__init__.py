@@ -672,11 +672,11 @@ class Handle:
             self._stream = s
 
     def _on_device(self, t, name):
+        if isinstance(t, torch.Tensor) and t.get_device() == self.device and t.is_contiguous():
+            return t.data_ptr()
         if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous()):
             raise FFTConvError(f"{name} must be a contiguous tensor in device memory")
-        if t.get_device() != self.device:
-            raise FFTConvError(f"{name} is on device {t.get_device()}, the handle on {self.device}")
-        return t.data_ptr()
+        raise FFTConvError(f"{name} is on device {t.get_device()}, the handle on {self.device}")
 
     def _typed(self, t, dtype, shape, name):
         p = self._on_device(t, name)
@@ -707,9 +707,10 @@ class Handle:
     @staticmethod
     def _feature_shape(tokens, D, planes, name):
         """(shape of features over these tokens, positions in a sample or 0)"""
-        s = tuple(tokens.shape)
+        s = tokens.shape
         if not planes:
-            return s + (D,), 0
+            return (*s, D), 0
+        s = tuple(s)
         if len(s) < 2:
             raise FFTConvError(f"planes need {name} of a sample dimension and at least one position dimension")
         T = 1
@@ -747,7 +748,7 @@ class Handle:
             raise FFTConvError("gy and tokens disagree")
         D = gy.shape[1 if planes else -1]
         shape, T = self._feature_shape(tokens, D, planes, "tokens")
-        if tuple(gy.shape) != shape:
+        if gy.shape != shape:
             raise FFTConvError("gy and tokens disagree")
         if gtable is None:
             if accumulate:
@@ -772,7 +773,7 @@ class Handle:
         V, D = wt.shape
         pt, bits = self._tokens(targets, "targets")
         shape, T = self._feature_shape(targets, D, planes, "targets")
-        if tuple(x.shape) != shape:
+        if x.shape != shape:
             raise FFTConvError("x, wt and targets disagree")
         return (k, px, pw, pt, bits), (targets.numel(), D, V, T)
 
