@@ -642,7 +642,7 @@ inline void thin_plan(XentPlan &p, int dtype, long N, int D, int V) {
     p.thin_blocks = (int)(want < places ? want : places);
 }
 
-constexpr size_t kPieceBytes = (size_t)256 << 20;
+constexpr size_t kPieceBytes = (size_t)640 << 20;
 
 inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool aligned) {
     XentPlan p{};
