@@ -2,6 +2,6 @@
 #include "xent_impl.hpp"
 
 namespace fc {
-hipError_t xent_fprop_f16(const XentCall &c, void *ws, hipStream_t s) { return Xent<_Float16, _Float16, false>(c, false, ws, s).fprop(); }
-hipError_t xent_backward_f16(const XentCall &c, void *ws, hipStream_t s) { return Xent<_Float16, _Float16, false>(c, true, ws, s).backward(); }
+hipError_t xent_fprop_f16(const XentCall &c, void *ws, hipStream_t s) { return Xent<_Float16>(c, false, ws, s).fprop(); }
+hipError_t xent_backward_f16(const XentCall &c, void *ws, hipStream_t s) { return Xent<_Float16>(c, true, ws, s).backward(); }
 }  // namespace fc

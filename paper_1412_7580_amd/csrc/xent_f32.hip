@@ -2,8 +2,8 @@
 #include "xent_impl.hpp"
 
 namespace fc {
-hipError_t xent_fprop_f32(const XentCall &c, void *ws, hipStream_t s) { return Xent<float, __bf16, true>(c, false, ws, s).fprop(); }
-hipError_t xent_backward_f32(const XentCall &c, void *ws, hipStream_t s) { return Xent<float, __bf16, true>(c, true, ws, s).backward(); }
+hipError_t xent_fprop_f32(const XentCall &c, void *ws, hipStream_t s) { return Xent<float>(c, false, ws, s).fprop(); }
+hipError_t xent_backward_f32(const XentCall &c, void *ws, hipStream_t s) { return Xent<float>(c, true, ws, s).backward(); }
 
 size_t xent_bytes(bool backward, int dtype, long N, int D, int V, bool aligned) {
     return N ? xent_plan(backward, dtype, N, D, V, aligned).total : 0;

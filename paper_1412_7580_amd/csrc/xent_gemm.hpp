@@ -13,9 +13,15 @@
 // 64 whole rows, and the transposing LDS reads turn them on their way to the matrix cores.  So G is
 // written once and nothing is transposed in memory.
 //
-// fp32 operands are three bf16 terms each (their cut is exact, see split2), side by side in the row: the
-// K loop walks six products of terms per 64 k, the small ones first.  What is left out is below 2^-24 of
-// the product of the two.
+// fp32 operands are terms side by side in the row, and the K loop walks products of terms per 64 k:
+//
+//  - The scores take two fp16 terms of values scaled row by row to below 2^15 by a power of two, which leaves
+//    the reduction as an exponent (of the row plus of the class): h = fp16(x), l = fp16(x - h), products l h,
+//    h l, h h.  A value is off by 2^-22 of itself or 2^-40 of its row's largest, and what is left out (l l) is
+//    2^-22 of a product: together less than fp32 sums of a few terms lose, at three products.
+//  - The gradients' products reduce over what has no scale of its own (a class's column of G may be tiny in all
+//    rows, and an optimizer will divide by its size): three bf16 terms, whose cut is exact (see split2), at six
+//    products.  What is left out is below 2^-24 of the product of the two.
 //
 // A tile is staged with direct global-to-LDS loads of 16 bytes a lane, one K step ahead, in two
 // buffers.  LDS is written in lane order, so the swizzle that spreads a column of 16-byte pieces over
@@ -59,11 +65,12 @@ struct GemmArgs {
     int places, most;        // rows: blocks the chip holds, steps-bound of the splits; they follow from the live rows
     // stats, grad
     const int *target;       // by row
+    const int *exp_m, *exp_n;    // two terms: exponents of the rows' and classes' scales
     float2 *part;            // [tiles_n][part_ld]: maximum and sum of a row's scores in a tile
     float *hit;              // the target's score, by row
     const float *lse, *coef; // by row
     int n0;                  // class of column 0
-    void *G;
+    void *G;                 // (from two terms: in three)
     long g_ld, g_term;
     long part_ld;
     // rows, classes
@@ -204,24 +211,26 @@ struct Tile {
     }
 };
 
-constexpr int xent_lds_bytes(int bm, int bn, int wn) { return 2 * (bm + bn) * 128 + 2 * 3 * bm * 4 + wn * bm * 8; }
+constexpr int xent_lds_bytes(int bm, int bn, int wn) { return 2 * (bm + bn) * 128 + 2 * (4 * bm + bn) * 4 + wn * bm * 8; }
 
 // Tiles of FM*WM*16 rows (m) by FN*WN*16 columns (n); a wave has FM*16 by FN*16 of one.  A block takes
 // tiles until there are none left: the next one's first two steps are on their way while the
 // last one's end is computed.
-template <class T, int FM, int FN, int WM, int WN, int END, bool SPLIT>
+template <class T, int FM, int FN, int WM, int WN, int END, int TERMS>
 __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
     constexpr int BM = FM * WM * 16, BN = FN * WN * 16, W = WM * WN;
     constexpr bool PIN = END != kClasses, QIN = END == kStats || END == kGrad;
-    constexpr int kRowValues = END == kStats ? 1 : END == kGrad ? 3 : 0;      // target, lse, coef
+    constexpr bool SCORES = END == kStats || END == kGrad;
+    constexpr int kProducts = TERMS == 3 ? 6 : TERMS == 2 ? 3 : 1;
     typedef typename Mfma<T>::frag F;
     typedef Tile<BM, W, PIN> TP;
     typedef Tile<BN, W, QIN> TQ;
     extern __shared__ __align__(1024) char lds[];
     constexpr int kBytes = (BM + BN) * 128;
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char *)lds;
-    char *const row_values = lds + 2 * kBytes;                                // [2][3][BM]
-    float2 *const both = reinterpret_cast<float2 *>(lds + 2 * kBytes + 2 * 3 * BM * 4);   // [WN][BM]
+    constexpr int kValues = 4 * BM + BN;                                      // of a tile: target, lse, coef, exponents of rows; of columns
+    char *const values = lds + 2 * kBytes;                                    // [2][kValues]
+    float2 *const both = reinterpret_cast<float2 *>(values + 2 * kValues * 4);    // [WN][BM]
 
     const int count = *a.count;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -231,8 +240,6 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
     const int total = tiles_m * a.tiles_n;
     const int splits = END == kRows ? rows_splits(total, a.places, a.most) : a.splits, units = total * splits;
     const int K = END == kClasses ? count : a.K, steps = (K + kStep - 1) / kStep;
-    constexpr int kTerms = SPLIT ? 6 : 1;
-
     TP tp;
     TQ tq;
     long m0, n0;
@@ -252,18 +259,20 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
         m0 = (long)(in / gn) * BM;
         n0 = (long)tn * BN;
         const int each = (steps + splits - 1) / splits, begin = split * each;
-        first = begin * kTerms;
-        last = (steps < begin + each ? steps : begin + each) * kTerms;
+        first = begin * kProducts;
+        last = (steps < begin + each ? steps : begin + each) * kProducts;
         tp.begin(a.P, m0, w, lane);
         tq.begin(a.Q, n0, w, lane);
     };
     auto stage = [&](int s) {
-        const int k0 = (SPLIT ? s / 6 : s) * kStep;
-        int tp_ = 0, tq_ = 0;                                // terms: l h, h l, m m, m h, h m, h h
-        if (SPLIT) {
-            const int t = s % 6;
+        const int t = s % kProducts, k0 = s / kProducts * kStep;
+        int tp_ = 0, tq_ = 0;
+        if (TERMS == 3) {                                    // l h, h l, m m, m h, h m, h h
             tp_ = t == 0 ? 2 : t == 2 || t == 3 ? 1 : 0;
             tq_ = t == 1 ? 2 : t == 2 || t == 4 ? 1 : 0;
+        } else if (TERMS == 2) {                             // l h, h l, h h
+            tp_ = t == 0;
+            tq_ = t == 1;
         }
         const unsigned to = lds0 + (s & 1) * kBytes;
         tp.load(a.P, a.zeros, k0, tp_, to, w, lane);
@@ -271,11 +280,19 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
     };
     // The first two steps, and before them the values that the tile's rows bring along.
     auto stage_first = [&](int parity) {
-        if constexpr (kRowValues > 0) {
-            for (int i = w; i < kRowValues * (BM / 64); i += W) {
-                const int which = i / (BM / 64), at = i % (BM / 64);
-                const void *from = which == 0 ? (const void *)(a.target + m0) : which == 1 ? (const void *)(a.lse + m0) : (const void *)(a.coef + m0);
-                lds_load4(uniform(static_cast<const char *>(from)), (at * 64 + lane) * 4, lds0 + 2 * kBytes + ((parity * 3 + which) * BM + at * 64) * 4);
+        if constexpr (SCORES) {
+            const auto fetch = [&](const void *from, int n, int to) {         // n values, 64 a wave and load
+                for (int i = w; i < n / 64; i += W)
+                    lds_load4(uniform(static_cast<const char *>(from)), (i * 64 + lane) * 4, lds0 + 2 * kBytes + (parity * kValues + to + i * 64) * 4);
+            };
+            fetch(a.target + m0, BM, 0);
+            if (END == kGrad) {
+                fetch(a.lse + m0, BM, BM);
+                fetch(a.coef + m0, BM, 2 * BM);
+            }
+            if (TERMS == 2) {
+                fetch(a.exp_m + m0, BM, 3 * BM);
+                fetch(a.exp_n + n0, BN, 4 * BM);
             }
         }
         if (first < last) stage(first);
@@ -353,8 +370,23 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
         int own = lane;
         asm volatile("" : "+v"(own));
         const int row = own & 15, quad = (own >> 4) * 4;
-        const int *targets = reinterpret_cast<const int *>(row_values + parity * 3 * BM * 4);
+        const int *targets = reinterpret_cast<const int *>(values + parity * kValues * 4);
         const float *lses = reinterpret_cast<const float *>(targets) + BM, *coefs = lses + BM;
+        if constexpr (SCORES && TERMS == 2) {
+            const int *exps = targets + 3 * BM;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int4 n = *reinterpret_cast<const int4 *>(exps + BM + (wn * FN + j) * 16 + quad);
+#pragma unroll
+                for (int i = 0; i < FM; ++i) {
+                    const int m = exps[(wm * FM + i) * 16 + row];
+                    acc[i][j][0] = ldexpf(acc[i][j][0], m + n.x);
+                    acc[i][j][1] = ldexpf(acc[i][j][1], m + n.y);
+                    acc[i][j][2] = ldexpf(acc[i][j][2], m + n.z);
+                    acc[i][j][3] = ldexpf(acc[i][j][3], m + n.w);
+                }
+            }
+        }
         if constexpr (END == kStats) {
             const bool edge = n_at + BN > a.N;
 #pragma unroll
@@ -403,7 +435,8 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
                 if (m_at + r < count) a.part[tn_at * a.part_ld + m_at + r] = v;
             }
         } else if constexpr (END == kGrad) {
-            T *G = static_cast<T *>(a.G);
+            constexpr int GT = TERMS == 1 ? 1 : 3;            // G's terms
+            T *G = static_cast<T *>(a.G);                    // (two bytes an element in any case)
             const bool edge = n_at + BN > a.N || m_at + BM > count;
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
@@ -415,17 +448,17 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
                 const bool any = __any(hit);
                 // Two column tiles at a time: lanes of odd sixteens trade theirs of the first tile for the second's of
                 // the sixteen before, after which a lane holds eight neighbouring columns of one of them.
-                const long m_ld = m * (SPLIT ? 3 * a.g_term : a.g_ld);
+                const long m_ld = m * (GT == 3 ? 3 * a.g_term : a.g_ld);
 #pragma unroll
                 for (int j = 0; j < FN; j += 2) {
-                    uint2 t[SPLIT ? 3 : 1][2];
+                    uint2 t[GT][2];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         float g[4];
                         // (for 16-bit operands one instruction less: off by the rounding of lse log2(e), as lse is by its own)
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            g[r] = SPLIT ? __expf(acc[i][j + h][r] - lse) : __builtin_amdgcn_exp2f(fmaf(acc[i][j + h][r], kLog2E, -lse2));
+                            g[r] = GT == 3 ? __expf(acc[i][j + h][r] - lse) : __builtin_amdgcn_exp2f(fmaf(acc[i][j + h][r], kLog2E, -lse2));
                         if (any)
 #pragma unroll
                             for (int r = 0; r < 4; ++r) g[r] -= hit && rel == (j + h) * 16 + r ? 1.f : 0.f;
@@ -436,7 +469,7 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
 #pragma unroll
                             for (int r = 0; r < 4; ++r) g[r] = m < count && n + r < a.N ? g[r] : 0.f;
                         }
-                        if constexpr (SPLIT) {
+                        if constexpr (GT == 3) {
                             split4(g[0], g[1], g[2], g[3], t[0][h], t[1][h], t[2][h]);
                         } else {
                             T v[4] = {(T)g[0], (T)g[1], (T)g[2], (T)g[3]};
@@ -446,7 +479,7 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
                     const long n = n_at + (wn * FN + j + (own >> 4 & 1)) * 16 + (own >> 5) * 8;
                     if (edge && (m >= a.M || n >= a.g_ld)) continue;
 #pragma unroll
-                    for (int q = 0; q < (SPLIT ? 3 : 1); ++q) {
+                    for (int q = 0; q < GT; ++q) {
                         const auto x = __builtin_amdgcn_permlane16_swap(t[q][0].x, t[q][1].x, false, false);
                         const auto y = __builtin_amdgcn_permlane16_swap(t[q][0].y, t[q][1].y, false, false);
                         *reinterpret_cast<uint4 *>(G + m_ld + q * a.g_term + n) = make_uint4(x[0], y[0], x[1], y[1]);
@@ -455,7 +488,7 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
             }
         } else {
             const float alpha = a.partial ? 1.f : *a.alpha_scale;
-            if constexpr (END == kClasses && !SPLIT) {
+            if constexpr (END == kClasses && TERMS == 1) {
                 // straight to 16-bit weights' gradients, 16 bytes a lane where their rows allow it
                 if (!a.partial && !a.add && a.out_ld % 8 == 0 && ((unsigned long)a.out & 15) == 0 && n_at + BN <= a.N) {
 #pragma unroll
@@ -509,7 +542,7 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
 #pragma unroll
                                 for (int r = 0; r < 4; ++r) if (r < left) out[r] = t[r];
                         };
-                        if constexpr (SPLIT) put(static_cast<float *>(a.out));
+                        if constexpr (TERMS == 3) put(static_cast<float *>(a.out));
                         else put(static_cast<T *>(a.out));
                     }
                 }

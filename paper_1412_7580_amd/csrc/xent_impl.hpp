@@ -157,51 +157,118 @@ __global__ __launch_bounds__(kThreads) void xent_place_kernel(ScanArgs a) {
 }
 
 // ---------------------------------------------------------------------------------- packing
-template <class S, class T, bool SPLIT>
+// Operands as the products read them: whole rows of a multiple of 8 elements, filled with zeros, the rows that
+// have a target only, and fp32 cut into terms.
+template <class S>
 struct PackArgs {
     const S *from;
-    T *to;                    // [rows][terms][ld]
+    S *to;                    // 16-bit types: [rows][ld]
+    _Float16 *two;            // fp32: [rows][2][ld], and the scales' exponents
+    __bf16 *three;            //       [rows][3][ld], where the gradients' products follow
+    int *exps;
     const int *row_of, *count;    // null: rows as they are
     long rows;                // rows behind the count are written as zeros
     int D, ld, T_;            // ld: a multiple of 8, filled with zeros
+    int lanes;                // fp32: threads of a row, a power of two up to 64
 };
 
-template <class T, bool SPLIT>
-__device__ __forceinline__ void put8(T *to, long term, const float (&f)[8]) {
-    if constexpr (SPLIT) {
-        uint4 h, m, l;
-        split2(f[0], f[1], h.x, m.x, l.x);
-        split2(f[2], f[3], h.y, m.y, l.y);
-        split2(f[4], f[5], h.z, m.z, l.z);
-        split2(f[6], f[7], h.w, m.w, l.w);
-        *reinterpret_cast<uint4 *>(to) = h;
-        *reinterpret_cast<uint4 *>(to + term) = m;
-        *reinterpret_cast<uint4 *>(to + 2 * term) = l;
-    } else {
-        T t[8];
+template <class T>
+__device__ __forceinline__ void put16(T *to, const T (&t)[8]) { __builtin_memcpy(__builtin_assume_aligned(to, 16), t, 16); }
+
+// The scale 2^-e takes a row whose largest value is `top` to below 2^15; rows that hold nothing but zeros, or
+// something that is not finite, stay.
+__device__ __forceinline__ int scale_exponent(float top) {
+    return top > 0.f && top < INFINITY ? __builtin_amdgcn_frexp_expf(top) - 15 : 0;
+}
+__device__ __forceinline__ void put_terms(const PackArgs<float> &a, long r, int d, const float (&f)[8], int e) {
+    _Float16 h[8], l[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = (T)f[i];
-        __builtin_memcpy(__builtin_assume_aligned(to, 16), t, 16);
+    for (int i = 0; i < 8; ++i) {
+        const float x = ldexpf(f[i], -e);
+        h[i] = (_Float16)x;
+        l[i] = (_Float16)(x - (float)h[i]);
+    }
+    _Float16 *const two = a.two + (size_t)r * 2 * a.ld + d;
+    put16(two, h);
+    put16(two + a.ld, l);
+    if (a.three) {
+        uint4 t[3];
+        split2(f[0], f[1], t[0].x, t[1].x, t[2].x);
+        split2(f[2], f[3], t[0].y, t[1].y, t[2].y);
+        split2(f[4], f[5], t[0].z, t[1].z, t[2].z);
+        split2(f[6], f[7], t[0].w, t[1].w, t[2].w);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(a.three + (size_t)r * 3 * a.ld + (size_t)q * a.ld + d) = t[q];
     }
 }
 
-template <class S, class T, bool SPLIT>
-__global__ __launch_bounds__(kThreads) void xent_pack_kernel(PackArgs<S, T, SPLIT> a) {
+template <class S>
+__global__ __launch_bounds__(kThreads) void xent_pack_kernel(PackArgs<S> a) {
     const long count = a.count ? *a.count : a.rows;
     const int cpr = a.ld / 8;
     const size_t total = (size_t)a.rows * cpr;
     for (size_t c = (size_t)blockIdx.x * kThreads + threadIdx.x; c < total; c += (size_t)gridDim.x * kThreads) {
         const long r = (long)(c / cpr);
         const int d = (int)(c - (size_t)r * cpr) * 8;
-        float f[8] = {};
-        if (r < count) load8(a.from + (size_t)(a.row_of ? a.row_of[r] : r) * a.D + d, a.D - d, f);
-        put8<T, SPLIT>(a.to + (size_t)r * a.ld * (SPLIT ? 3 : 1) + d, a.ld, f);
+        S t[8] = {};
+        if (r < count) raw8(a.from + (size_t)(a.row_of ? a.row_of[r] : r) * a.D + d, a.D - d, t);
+        put16(a.to + (size_t)r * a.ld + d, t);
     }
 }
 
-template <class S, class T, bool SPLIT>
-__global__ __launch_bounds__(kThreads) void xent_pack_planes_kernel(PackArgs<S, T, SPLIT> a) {
-    __shared__ float tile[64][65];
+// fp32: a.lanes threads find a row's largest value, then cut it (it is still in the cache).
+__global__ __launch_bounds__(kThreads) void xent_cut_kernel(PackArgs<float> a) {
+    const long count = a.count ? *a.count : a.rows;
+    const int l = threadIdx.x % a.lanes, rows = kThreads / a.lanes;
+    for (long r0 = (long)blockIdx.x * rows; r0 < a.rows; r0 += (long)gridDim.x * rows) {
+        const long r = r0 + threadIdx.x / a.lanes;
+        if (r >= a.rows) return;
+        const float *const from = r < count ? a.from + (size_t)(a.row_of ? a.row_of[r] : r) * a.D : nullptr;
+        float top = 0.f;
+        if (from)
+            for (int d = l * 8; d < a.D; d += a.lanes * 8) {
+                float f[8];
+                load8(from + d, a.D - d, f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[i]));
+            }
+        for (int m = 1; m < a.lanes; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+        const int e = scale_exponent(top);
+        if (l == 0) a.exps[r] = e;
+        for (int d = l * 8; d < a.ld; d += a.lanes * 8) {
+            float f[8] = {};
+            if (from) load8(from + d, a.D - d, f);
+            put_terms(a, r, d, f, e);
+        }
+    }
+}
+
+// The largest value of each packed row that lies in planes: 64 rows a block, a quarter of the planes a wave.
+__global__ __launch_bounds__(kThreads) void xent_planes_top_kernel(PackArgs<float> a) {
+    __shared__ float tops[4][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const long r = (long)blockIdx.x * 64 + lane;
+    float top = 0.f;
+    if (r < *a.count) {
+        const RowsOf at{a.D, a.T_};
+        const float *const p = a.from + at.offset(a.row_of[r]);
+        constexpr int U = 16;
+        for (int d = w; d < a.D; d += 4 * U) {
+            float v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = p[(size_t)(d + 4 * u < a.D ? d + 4 * u : d) * a.T_];
+#pragma unroll
+            for (int u = 0; u < U; ++u) top = fmaxf(top, fabsf(v[u]));
+        }
+    }
+    tops[w][lane] = top;
+    __syncthreads();
+    if (w == 0 && r < a.rows) a.exps[r] = scale_exponent(fmaxf(fmaxf(tops[0][lane], tops[1][lane]), fmaxf(tops[2][lane], tops[3][lane])));
+}
+
+template <class S>
+__global__ __launch_bounds__(kThreads) void xent_pack_planes_kernel(PackArgs<S> a) {
+    __shared__ S tile[64][sizeof(S) == 4 ? 65 : 66];
     const long count = *a.count;
     const unsigned tiles_d = (a.D + 63) / 64;
     const long r0 = (long)(blockIdx.x / tiles_d) * 64;
@@ -217,18 +284,19 @@ __global__ __launch_bounds__(kThreads) void xent_pack_planes_kernel(PackArgs<S, 
             v[i] = p[(size_t)(d < a.D ? d : a.D - 1) * a.T_];
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) tile[i * 4 + w][lane] = d0 + i * 4 + w < a.D ? to_float(v[i]) : 0.f;
+        for (int i = 0; i < 16; ++i) tile[i * 4 + w][lane] = d0 + i * 4 + w < a.D ? v[i] : (S)0.f;
     } else {
-        for (int i = w; i < 64; i += 4) tile[i][lane] = 0.f;
+        for (int i = w; i < 64; i += 4) tile[i][lane] = (S)0.f;
     }
     __syncthreads();
     for (int c = threadIdx.x; c < 64 * 8; c += kThreads) {
         const int q = c >> 3, dd = (c & 7) * 8;
         if (d0 + dd >= a.ld || r0 + q >= a.rows) continue;
-        float f[8];
+        S t[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = tile[dd + i][q];
-        put8<T, SPLIT>(a.to + (size_t)(r0 + q) * a.ld * (SPLIT ? 3 : 1) + d0 + dd, a.ld, f);
+        for (int i = 0; i < 8; ++i) t[i] = tile[dd + i][q];
+        if constexpr (sizeof(S) == 4) put_terms(a, r0 + q, d0 + dd, t, a.exps[r0 + q]);
+        else put16(a.to + (size_t)(r0 + q) * a.ld + d0 + dd, t);
     }
 }
 
@@ -614,13 +682,13 @@ inline Shape shape_of(long M, long N, long K, int terms, bool split) {
 struct XentPlan {
     long Np;                  // rows, up to a multiple of 256
     int Dp, Dc;               // features, up to a multiple of 8 and of 4
-    int terms;
+    int terms;                // of fp32 in the gradients' products
     bool pack_w;
     int thin_tiles, thin_blocks, thin_lds;    // tiles of 16 rows in a block (0: not that path), blocks of a group of rows
     int piece, pieces;        // classes a piece
     Shape score, rows, classes;
     int scan_blocks;
-    size_t row_of, pos, target, count, counts, tops, lse, coef, hit, part, x, w, G, gx, gw, total;
+    size_t row_of, pos, target, count, counts, tops, lse, coef, hit, part, x, w, x3, w3, ex, ew, G, gx, gw, total;
 };
 
 // Few rows: as many tiles of 16 of them as a block's LDS holds, four at most.  More groups of rows read the
@@ -666,8 +734,13 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
     p.scan_blocks = (int)((N + kScanRows - 1) / kScanRows);
     p.counts = take((size_t)p.scan_blocks * 4);
     p.tops = take((size_t)p.scan_blocks * 4);
-    p.x = take((size_t)p.Np * p.terms * p.Dp * 2);
-    p.w = take(p.pack_w ? (size_t)V * p.terms * p.Dp * 2 : 0);
+    const size_t cut = dtype == kF32 ? 2 : 1;            // terms in the scores' product
+    p.x = take((size_t)p.Np * cut * p.Dp * 2);
+    p.w = take(p.pack_w ? (size_t)V * cut * p.Dp * 2 : 0);
+    p.ex = take(cut == 2 ? (size_t)p.Np * 4 : 0);
+    p.ew = take(cut == 2 ? (size_t)ceil_to(V, 256) * 4 : 0);
+    p.x3 = take(backward && cut == 2 ? (size_t)p.Np * 3 * p.Dp * 2 : 0);
+    p.w3 = take(backward && cut == 2 ? (size_t)V * 3 * p.Dp * 2 : 0);
     if (!backward) {
         p.score = shape_of(N, V, D, p.terms, false);
         p.hit = take((size_t)N * 4);
@@ -696,7 +769,7 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
     return p;
 }
 
-template <class T, int END, bool SPLIT>
+template <class T, int END, int TERMS>
 hipError_t product(GemmArgs &g, const Shape &sh, hipStream_t s) {
     g.tiles_m = sh.tiles_m; g.tiles_n = sh.tiles_n; g.splits = sh.splits;
     g.places = (int)places(sh); g.most = sh.most;
@@ -708,9 +781,9 @@ hipError_t product(GemmArgs &g, const Shape &sh, hipStream_t s) {
         return hipGetLastError();
     };
     if constexpr (END == kRows || END == kClasses)
-        if (sh.bn == 192) return launch(xent_gemm_kernel<T, 4, 6, 4, 2, END, SPLIT>, 512, xent_lds_bytes(256, 192, 2));
-    if (sh.bm == 256) return launch(xent_gemm_kernel<T, 4, 8, 4, 2, END, SPLIT>, 512, xent_lds_bytes(256, 256, 2));
-    return launch(xent_gemm_kernel<T, 4, 4, 2, 2, END, SPLIT>, 256, xent_lds_bytes(128, 128, 2));
+        if (sh.bn == 192) return launch(xent_gemm_kernel<T, 4, 6, 4, 2, END, TERMS>, 512, xent_lds_bytes(256, 192, 2));
+    if (sh.bm == 256) return launch(xent_gemm_kernel<T, 4, 8, 4, 2, END, TERMS>, 512, xent_lds_bytes(256, 256, 2));
+    return launch(xent_gemm_kernel<T, 4, 4, 2, 2, END, TERMS>, 256, xent_lds_bytes(128, 128, 2));
 }
 
 inline unsigned blocks_for(size_t chunks) {
@@ -727,9 +800,16 @@ inline bool xent_launchable(const XentPlan &p, bool backward, long N, int D, int
     return backward ? product(p.score) && product(p.rows) && product(p.classes) : product(p.score);
 }
 
-// S: the operands' type in memory; T: the type the matrix cores take.
-template <class S, class T, bool SPLIT>
+// S: the operands' type in memory.  The matrix cores take Score for the scores and Grad for the gradients, in
+// so many terms.
+template <class S> struct Cores { typedef S Score, Grad; static constexpr int score = 1, grad = 1; };
+template <> struct Cores<float> { typedef _Float16 Score; typedef __bf16 Grad; static constexpr int score = 2, grad = 3; };
+
+template <class S>
 struct Xent {
+    typedef typename Cores<S>::Score Score;
+    typedef typename Cores<S>::Grad Grad;
+    static constexpr int kScore = Cores<S>::score, kGradTerms = Cores<S>::grad;
     const XentCall &c;
     const XentPlan p;
     char *ws;
@@ -749,25 +829,45 @@ struct Xent {
         if (sc.blocks > kScanInline) hipLaunchKernelGGL(xent_count_kernel, dim3(sc.blocks), dim3(kThreads), 0, s, sc);
         hipLaunchKernelGGL(xent_place_kernel, dim3(sc.blocks), dim3(kThreads), 0, s, sc);
     }
-    hipError_t pack() {
-        PackArgs<S, T, SPLIT> a{static_cast<const S *>(c.x), at<T>(p.x), at<int>(p.row_of), at<int>(p.count), p.Np, c.D, p.Dp, c.T};
-        if (c.T) {
-            const long blocks = p.Np / 64 * ((c.D + 63) / 64);
-            hipLaunchKernelGGL((xent_pack_planes_kernel<S, T, SPLIT>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+    hipError_t pack(bool backward) {
+        PackArgs<S> a{};
+        a.from = static_cast<const S *>(c.x); a.row_of = at<int>(p.row_of); a.count = at<int>(p.count);
+        a.rows = p.Np; a.D = c.D; a.ld = p.Dp; a.T_ = c.T;
+        PackArgs<S> b{};
+        b.from = static_cast<const S *>(c.wt); b.rows = c.V; b.D = c.D; b.ld = p.Dp;
+        if constexpr (kScore == 2) {
+            a.two = at<_Float16>(p.x); a.exps = at<int>(p.ex);
+            b.two = at<_Float16>(p.w); b.exps = at<int>(p.ew);
+            if (backward) { a.three = at<__bf16>(p.x3); b.three = at<__bf16>(p.w3); }
+            a.lanes = 1;
+            while (a.lanes < 64 && a.lanes * 8 < p.Dp) a.lanes *= 2;
+            b.lanes = a.lanes;
+            if (c.T) {
+                hipLaunchKernelGGL(xent_planes_top_kernel, dim3((unsigned)(p.Np / 64)), dim3(kThreads), 0, s, a);
+                hipLaunchKernelGGL(xent_pack_planes_kernel<S>, dim3((unsigned)(p.Np / 64 * ((c.D + 63) / 64))), dim3(kThreads), 0, s, a);
+            } else {
+                hipLaunchKernelGGL(xent_cut_kernel, dim3(blocks_for((size_t)p.Np * a.lanes)), dim3(kThreads), 0, s, a);
+            }
+            hipLaunchKernelGGL(xent_cut_kernel, dim3(blocks_for((size_t)c.V * b.lanes)), dim3(kThreads), 0, s, b);
         } else {
-            hipLaunchKernelGGL((xent_pack_kernel<S, T, SPLIT>), dim3(blocks_for((size_t)p.Np * p.Dp / 8)), dim3(kThreads), 0, s, a);
-        }
-        if (p.pack_w) {
-            PackArgs<S, T, SPLIT> b{static_cast<const S *>(c.wt), at<T>(p.w), nullptr, nullptr, c.V, c.D, p.Dp, 0};
-            hipLaunchKernelGGL((xent_pack_kernel<S, T, SPLIT>), dim3(blocks_for((size_t)c.V * p.Dp / 8)), dim3(kThreads), 0, s, b);
+            a.to = at<S>(p.x);
+            b.to = at<S>(p.w);
+            if (c.T) hipLaunchKernelGGL(xent_pack_planes_kernel<S>, dim3((unsigned)(p.Np / 64 * ((c.D + 63) / 64))), dim3(kThreads), 0, s, a);
+            else hipLaunchKernelGGL(xent_pack_kernel<S>, dim3(blocks_for((size_t)p.Np * p.Dp / 8)), dim3(kThreads), 0, s, a);
+            if (p.pack_w) hipLaunchKernelGGL(xent_pack_kernel<S>, dim3(blocks_for((size_t)c.V * p.Dp / 8)), dim3(kThreads), 0, s, b);
         }
         return hipGetLastError();
     }
-    GemmSide features() const { return GemmSide{at<T>(p.x), (long)p.terms * p.Dp, p.Dp, p.Np, p.Dp}; }
+    // Features and weights (from class v0 on) as the scores' product reads them, and as the gradients' do.
+    GemmSide features() const { return GemmSide{at<Score>(p.x), (long)kScore * p.Dp, p.Dp, p.Np, p.Dp}; }
     GemmSide weights(long v0) const {
-        const long ld = (long)p.terms * p.Dp;
-        const T *w = p.pack_w ? at<T>(p.w) : static_cast<const T *>(c.wt);
+        const long ld = (long)kScore * p.Dp;
+        const Score *w = p.pack_w ? at<Score>(p.w) : static_cast<const Score *>(c.wt);
         return GemmSide{w + v0 * ld, ld, p.Dp, c.V - v0, p.Dp};
+    }
+    GemmSide grad_features() const { return kGradTerms == 1 ? features() : GemmSide{at<Grad>(p.x3), 3L * p.Dp, p.Dp, p.Np, p.Dp}; }
+    GemmSide grad_weights(long v0) const {
+        return kGradTerms == 1 ? weights(v0) : GemmSide{at<Grad>(p.w3) + v0 * 3 * p.Dp, 3L * p.Dp, p.Dp, c.V - v0, p.Dp};
     }
 
     template <int NT>
@@ -788,13 +888,14 @@ struct Xent {
         ScanArgs sc{};
         sc.loss = c.loss; sc.lse = c.lse;
         scan(sc);
-        if (hipError_t e = pack(); e != hipSuccess) return e;
+        if (hipError_t e = pack(false); e != hipSuccess) return e;
         GemmArgs g{};
         g.P = features(); g.Q = weights(0);
+        g.exp_m = at<int>(p.ex); g.exp_n = at<int>(p.ew);
         g.count = sc.count; g.zeros = zeros();
         g.M = (int)p.Np; g.N = c.V; g.K = c.D;
         g.target = sc.target; g.part = at<float2>(p.part); g.part_ld = p.Np; g.hit = at<float>(p.hit);
-        if (hipError_t e = product<T, kStats, SPLIT>(g, p.score, s); e != hipSuccess) return e;
+        if (hipError_t e = product<Score, kStats, kScore>(g, p.score, s); e != hipSuccess) return e;
         const LossArgs l{g.part, p.Np, p.score.tiles_n, g.hit, sc.row_of, sc.count, c.loss, c.lse};
         hipLaunchKernelGGL(xent_loss_kernel, dim3((unsigned)(p.Np / 64)), dim3(1024), 0, s, l);
         return hipGetLastError();
@@ -808,32 +909,33 @@ struct Xent {
         sc.alpha = at<float>(p.count + 4);
         sc.scale = c.scale; sc.mean = c.mean; sc.half_range = c.dtype == kF16;
         scan(sc);
-        if (hipError_t e = pack(); e != hipSuccess) return e;
+        if (hipError_t e = pack(true); e != hipSuccess) return e;
         for (int i = 0; i < p.pieces; ++i) {
             const long v0 = (long)i * p.piece;
             const int width = (int)(c.V - v0 < p.piece ? c.V - v0 : p.piece);
             const long ld = ceil_to(width, 64);
-            const GemmSide G{at<T>(p.G), p.terms * ld, ld, p.Np, (int)ld};
+            const GemmSide G{at<Grad>(p.G), p.terms * ld, ld, p.Np, (int)ld};
             GemmArgs g{};
             g.P = features(); g.Q = weights(v0);
+            g.exp_m = at<int>(p.ex); g.exp_n = at<int>(p.ew) + v0;
             g.count = sc.count; g.zeros = zeros();
             g.M = (int)p.Np; g.N = width; g.K = c.D;
             g.target = sc.target; g.lse = sc.lse_out; g.coef = sc.coef;
             g.n0 = (int)v0;
-            g.G = at<T>(p.G); g.g_ld = ld; g.g_term = ld;
-            if (hipError_t e = product<T, kGrad, SPLIT>(g, tiles(p.score, c.N, width), s); e != hipSuccess) return e;
+            g.G = at<Grad>(p.G); g.g_ld = ld; g.g_term = ld;
+            if (hipError_t e = product<Score, kGrad, kScore>(g, tiles(p.score, c.N, width), s); e != hipSuccess) return e;
             if (c.gx) {
                 GemmArgs r{};
-                r.P = G; r.Q = weights(v0);
+                r.P = G; r.Q = grad_weights(v0);
                 r.count = sc.count; r.zeros = zeros();
                 r.M = (int)p.Np; r.N = c.D; r.K = width;
                 r.partial = at<float>(p.gx); r.part_cols = p.Dc; r.add = i > 0;
                 r.alpha_scale = sc.alpha;
-                if (hipError_t e = product<T, kRows, SPLIT>(r, p.rows, s); e != hipSuccess) return e;
+                if (hipError_t e = product<Grad, kRows, kGradTerms>(r, p.rows, s); e != hipSuccess) return e;
             }
             if (c.gw) {
                 GemmArgs w{};
-                w.P = G; w.Q = features();
+                w.P = G; w.Q = grad_features();
                 w.count = sc.count; w.zeros = zeros();
                 w.M = width; w.N = c.D; w.K = (int)c.N;
                 w.alpha_scale = sc.alpha;
@@ -841,7 +943,7 @@ struct Xent {
                 const Shape sh = tiles(p.classes, width, c.D);
                 if (sh.splits > 1) { w.partial = at<float>(p.gw); w.part_cols = p.Dc; }
                 else { w.out = gw; w.out_ld = c.D; w.add = c.accumulate; }
-                if (hipError_t e = product<T, kClasses, SPLIT>(w, sh, s); e != hipSuccess) return e;
+                if (hipError_t e = product<Grad, kClasses, kGradTerms>(w, sh, s); e != hipSuccess) return e;
                 if (sh.splits > 1) {
                     const ClassesOutArgs<S> o{at<float>(p.gw), sc.alpha, gw, width, p.Dc, sh.splits, c.D, c.accumulate};
                     hipLaunchKernelGGL(xent_classes_out_kernel<S>, dim3(blocks_for((size_t)width * ((c.D + 7) / 8))), dim3(kThreads), 0, s, o);
