@@ -213,7 +213,10 @@ struct Tile {
 
 constexpr int xent_lds_bytes(int bm, int bn, int wn) { return 2 * (bm + bn) * 128 + 2 * (4 * bm + bn) * 4 + wn * bm * 8; }
 
-// Tiles of FM*WM*16 rows (m) by FN*WN*16 columns (n); a wave has FM*16 by FN*16 of one.  A block takes
+// Tiles of FM*WM*16 rows (m) by FN*WN*16 columns (n); a wave has FM*16 by FN*16 of one.  256x256 tiles of eight
+// waves: 128 of a wave's 256 registers are sums, two half steps of fragments 96.  (Four waves of 128x128 spill;
+// two blocks a CU of 128x256 tiles in steps of 32 k hide each other's ends but stage half as much again: 7.9 ms
+// instead of 6.97 for the step of 8192 rows; 32x32 matrix instructions 8 % slower, and wave priorities 5 %.)  A block takes
 // tiles until there are none left: the next one's first two steps are on their way while the
 // last one's end is computed.
 template <class T, int FM, int FN, int WM, int WN, int END, int TERMS>
@@ -366,7 +369,8 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
             stage_first(parity ^ 1);
         }
 
-        // A lane holds, of each 16x16 tile, row lane & 15 and the four columns from 4 (lane >> 4) on.
+        // A lane holds, of each 16x16 tile, row lane & 15 and the four columns from 4 (lane >> 4) on.  (The ends are
+        // vector work, 6 us of a tile's 35 at 1024 features, half of it exponentials.)
         int own = lane;
         asm volatile("" : "+v"(own));
         const int row = own & 15, quad = (own >> 4) * 4;

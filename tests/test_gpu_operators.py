@@ -5,7 +5,9 @@ operands' type (2^-8, 2^-11, 2^-24), e = 2^-24 half a step of fp32.
   - A sum of n products in fp32, in any order, is off by at most n e times the sum of their sizes.
   - exp of a difference t in fp32: t is off by e |t| and its product with log2(e) again, the hardware's power of
     two by a step: at most (3 |t| + 4) e of the result.
-  - What is rounded to the operands' type is off by u of itself, or half its smallest step if that is more."""
+  - What is rounded to the operands' type is off by u of itself, or half its smallest step if that is more.
+  - fp32 scores are formed from two fp16 terms of each value: 2^-22 of x, of w, and of their product for what is left
+    out, 12 e of |x w| in all, and three products a term in the sum."""
 import math
 
 import pytest
@@ -138,7 +140,8 @@ def xent_reference(x, w, tokens, gloss, scale, mean, planes):
     W = w.double()
     z = X @ W.t()
     lse = torch.logsumexp(z, 1)
-    dz = ((terms * D + 8) * E * (X.abs() @ W.abs().t())).amax(1)     # a score's error, the largest of its row
+    cut = 12 if dtype == torch.float32 else 0
+    dz = ((terms * D + 8 + cut) * E * (X.abs() @ W.abs().t())).amax(1)     # a score's error, the largest of its row
     span = (z.amax(1) - z.amin(1)).clamp(max=100.0)          # (smaller terms do not count)
     dlse = dz + (3 * span + 4 + V ** 0.5 + 300) * E + 2 * E * lse.abs()
     loss = lse - z.gather(1, at[:, None])[:, 0]
@@ -319,6 +322,93 @@ def test_xent_gradients_against_differences(hd):
     exactly = float(ref["gx"][1].mul(dx.abs()).sum() + ref["gw"][1].mul(dw.abs()).sum())
     assert abs(float(up - down) / (2 * h) - slope) <= h * h / 6 * third + noise + exactly
     assert h * h / 6 * third + noise + exactly < 0.2 * abs(slope) + 0.2
+
+
+@pytest.mark.parametrize("ex,ew", [(0, 0), (-100, 100), (60, -60), (-120, 118), (-126, 120)])
+def test_xent_fp32_rows_of_any_scale(hd, ex, ew):
+    """Features around 2^ex, weights around 2^ew, each row spread over 2^12: the scores' two fp16 terms are scaled row by
+    row.  A value is off by 2^-22 of itself or 2^-40 of its row's largest, products by three such errors."""
+    g = gen(50)
+    N, D, V = 500, 200, 1500
+    x = torch.randn(N, D, generator=g, device="cuda") * torch.exp2(torch.randint(-12, 1, (N, D), generator=g, device="cuda").float())
+    w = torch.randn(V, D, generator=g, device="cuda") / math.sqrt(D)
+    x, w = torch.ldexp(x, torch.tensor(ex, device="cuda")), torch.ldexp(w, torch.tensor(ew, device="cuda"))
+    tokens = tokens_for(g, (N,), V)
+    ref = xent_reference(x, w, tokens, None, 1.0, False, False)
+    has, _ = picks(tokens, V)
+    X, W = x.double().abs() * has[:, None], w.double().abs()
+    more = 3 * 2.0 ** -40 * (X.amax(1) * W.sum(1).max() + X.sum(1) * W.max()) + 2.0 ** -126
+    loss, lse = hd.xent_fprop(x, w, tokens)
+    within(loss, ref["loss"][0], ref["loss"][1] + 3 * more, "loss")
+    within(lse, ref["lse"][0], ref["lse"][1] + 2 * more, "lse")
+
+
+def test_xent_fp32_of_a_tiny_class(hd):
+    """A class that no row comes near: its gradient is small in every row, and as exact as the others'."""
+    g = gen(51)
+    N, D, V = 300, 48, 200
+    x = torch.randn(N, D, generator=g, device="cuda").abs()
+    w = torch.randn(V, D, generator=g, device="cuda") * 0.1
+    w[7] = -0.6                                             # p of about e^-20
+    tokens = torch.full((N,), 3, dtype=torch.int64, device="cuda")
+    _, lse = hd.xent_fprop(x, w, tokens)
+    _, gw = hd.xent_backward(x, w, tokens, lse, want_gx=False)
+    ref = xent_reference(x, w, tokens, None, 1.0, False, False)["gw"]
+    within(gw, *ref, "gw")
+    assert 0 < float(ref[0][7].max()) < 1e-3 and bool((ref[1][7] < 1e-3 * ref[0][7]).all())
+
+
+def test_capture_without_an_eager_call_before(lib):
+    h = lib.Handle(0)
+    try:
+        g = gen(52)
+        x, w = torch.randn(700, 128, generator=g, device="cuda").bfloat16(), torch.randn(5000, 128, generator=g, device="cuda").bfloat16()
+        t = tokens_for(g, (700,), 5000)
+        ws = [torch.empty(h.xent_workspace_bytes(k, x.dtype, 700, 128, 5000), dtype=torch.uint8, device="cuda") for k in (lib.FPROP, lib.BPROP)]
+        loss, lse = torch.empty(700, device="cuda"), torch.empty(700, device="cuda")
+        gx, gw = torch.empty_like(x), torch.empty_like(w)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            h.xent_fprop(x, w, t, loss=loss, lse=lse, ws=ws[0])
+            h.xent_backward(x, w, t, lse, gx=gx, gw=gw, ws=ws[1])
+        for _ in range(3):
+            for v in (loss, gx, gw):
+                v.fill_(7)
+            graph.replay()
+            torch.cuda.synchronize()
+            want = h.xent_fprop(x, w, t)
+            wg = h.xent_backward(x, w, t, want[1])
+            assert torch.equal(loss, want[0]) and torch.equal(gx, wg[0]) and torch.equal(gw, wg[1])
+    finally:
+        h.close()
+
+
+@pytest.mark.parametrize("seed", range(30))
+def test_random_sizes(hd, seed):
+    import random
+    rng = random.Random(seed)
+
+    def size(lo, hi):
+        return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+    dtype, N, D, V = TYPES[seed % 3], size(1, 3000), size(1, 700), size(1, 9000)
+    planes = rng.random() < 0.3
+    T = size(1, 200)
+    shape = (max(1, N // T), T) if planes else (N,)
+    g = gen(seed)
+    tokens = tokens_for(g, shape, V, none=rng.choice([0, 0.1, 0.5, 0.95]), dtype=rng.choice([torch.int32, torch.int64]))
+    x = torch.randn((shape[0], D) + shape[1:] if planes else shape + (D,), generator=g, device="cuda").to(dtype)
+    w = (torch.randn(V, D, generator=g, device="cuda") * rng.choice([0.1, 2, 8]) / math.sqrt(D)).to(dtype)
+    gloss = torch.randn(shape, generator=g, device="cuda") if rng.random() < 0.5 else None
+    mean, scale = rng.random() < 0.5, 64.0 if dtype == torch.float16 else 1.0
+    ref = xent_reference(x, w, tokens, gloss, scale, mean, planes)
+    loss, lse = hd.xent_fprop(x, w, tokens, planes=planes)
+    within(loss.reshape(-1), *ref["loss"], "loss")
+    within(lse.reshape(-1), *ref["lse"], "lse")
+    gx, gw = hd.xent_backward(x, w, tokens, lse, gloss=gloss, scale=scale, mean=mean, planes=planes)
+    within(rows_of(gx, planes), *ref["gx"], "gx")
+    within(gw, *ref["gw"], "gw")
 
 
 def test_xent_beyond_32_bit_offsets(hd):
