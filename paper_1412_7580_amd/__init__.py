@@ -731,7 +731,7 @@ class Handle:
         t, bits = self._tokens(tokens, "tokens")
         shape, T = self._feature_shape(tokens, D, planes, "tokens")
         if y is None:
-            y = torch.empty(shape, device=table.device, dtype=table.dtype)
+            y = table.new_empty(shape)
             to = y.data_ptr()
         else:
             to = self._typed(y, table.dtype, shape, "y")
@@ -753,7 +753,7 @@ class Handle:
         if gtable is None:
             if accumulate:
                 raise FFTConvError("accumulate needs an existing gtable")
-            gtable = torch.empty((V, D), device=gy.device, dtype=gy.dtype)
+            gtable = gy.new_empty((V, D))
             to = gtable.data_ptr()
         else:
             to = self._typed(gtable, gy.dtype, (V, D), "gtable")
@@ -785,7 +785,7 @@ class Handle:
         outs = []
         for t, name in ((loss, "loss"), (lse, "lse")):
             if t is None:
-                t = torch.empty(targets.shape, device=x.device, dtype=torch.float32)
+                t = x.new_empty(targets.shape, dtype=torch.float32)
                 outs.append((t, t.data_ptr()))
             else:
                 outs.append((t, self._typed(t, torch.float32, targets.shape, name)))
@@ -830,16 +830,16 @@ class Handle:
             pointers[i], sizes[i], kinds[i] = t.data_ptr(), t.numel(), k
         return n, pointers, sizes, kinds
 
-    def _norm_result(self, norm):
+    def _norm_result(self, grads, norm):
         if norm is None:
-            norm = torch.empty((), device=f"cuda:{self.device}", dtype=torch.float32)
+            norm = grads[0].new_empty((), dtype=torch.float32) if grads else torch.empty((), device=f"cuda:{self.device}")
             return norm, norm.data_ptr()
         return norm, self._typed(norm, torch.float32, (), "norm")
 
     def grad_norm(self, grads, norm=None, ws=None):
         """The 2-norm of a list of tensors taken together, as a float32 tensor on the device."""
         args = self._tensor_list(grads)
-        norm, to = self._norm_result(norm)
+        norm, to = self._norm_result(grads, norm)
         self._device_stream()
         _check(self._lib.fftconv_grad_norm(self._h, *args, to, *self._scratch(ws)), "fftconv_grad_norm")
         return norm
@@ -853,7 +853,7 @@ class Handle:
             if len(out) != len(grads):
                 raise FFTConvError("out and the gradients disagree")
             to = (ctypes.c_void_p * len(out))(*[self._typed(o, t.dtype, t.shape, "out") for o, t in zip(out, grads)])
-        norm, pn = self._norm_result(norm)
+        norm, pn = self._norm_result(grads, norm)
         self._device_stream()
         _check(self._lib.fftconv_grad_clip(self._h, *args, to, float(max_norm), pn, *self._scratch(ws)), "fftconv_grad_clip")
         return norm

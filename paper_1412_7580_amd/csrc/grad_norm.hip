@@ -20,15 +20,16 @@ namespace fc {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPerLaunch = 128;          // tensors in one launch's arguments (29 bytes each, of 4096)
+constexpr int kPerLaunch = 128, kFew = 16;    // tensors in one launch's arguments (29 bytes each, of 4096), and in a short list's
 constexpr long kPieces = 2048, kLeast = 8192;      // eight blocks a CU, none of them tiny
 
+template <int CAP>
 struct NormArgs {
-    const void *in[kPerLaunch];
-    void *out[kPerLaunch];
-    long size[kPerLaunch];
-    int first[kPerLaunch + 1];           // number of the tensor's first piece within this launch
-    unsigned char dtype[kPerLaunch];
+    const void *in[CAP];
+    void *out[CAP];
+    long size[CAP];
+    int first[CAP + 1];                  // number of the tensor's first piece within this launch
+    unsigned char dtype[CAP];
     int count, base;                     // tensors, pieces of earlier launches
     long piece;                          // elements, a multiple of 8
     double *sums;
@@ -37,7 +38,8 @@ struct NormArgs {
     float max_norm;
 };
 
-__device__ __forceinline__ int tensor_of(const NormArgs &a, int p) {
+template <int CAP>
+__device__ __forceinline__ int tensor_of(const NormArgs<CAP> &a, int p) {
     int lo = 0, hi = a.count;            // the last tensor whose first piece is not behind p
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
@@ -77,7 +79,8 @@ __device__ __forceinline__ double squares(const T *p, long n) {
     return s;
 }
 
-__global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a) {
+template <int CAP>
+__global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs<CAP> a) {
     __shared__ double lds[4];
     const int p = blockIdx.x, t = tensor_of(a, p);
     const long from = (long)(p - a.first[t]) * a.piece;
@@ -128,7 +131,8 @@ __device__ __forceinline__ void scaled(const T *in, T *out, long n, float c) {
 }
 
 // The pieces are walked from the last one back: the end of what the norm read is still in the cache.
-__global__ __launch_bounds__(kThreads) void clip_kernel(NormArgs a) {
+template <int CAP>
+__global__ __launch_bounds__(kThreads) void clip_kernel(NormArgs<CAP> a) {
     __shared__ double lds[4];
     const double norm = sqrt(total(a.sums, a.pieces, lds));
     if (a.base == 0 && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
@@ -155,17 +159,11 @@ long pieces_of(int count, const long *sizes, long piece) {
     return n;
 }
 
-}  // namespace
-
-size_t grad_norm_bytes(int count, const long *sizes) {
-    return up((size_t)pieces_of(count, sizes, piece_length(count, sizes)) * sizeof(double), 256);
-}
-
-hipError_t launch_grad_norm(int count, const void *const *grads, const long *sizes, const int *dtypes, void *const *out,
-                            float max_norm, float *norm, void *ws, hipStream_t s) {
-    NormArgs a;
-    a.piece = piece_length(count, sizes);
-    const long pieces = pieces_of(count, sizes, a.piece);
+template <int CAP>
+void launch(int count, const void *const *grads, const long *sizes, const int *dtypes, void *const *out, float max_norm,
+            float *norm, void *ws, long piece, long pieces, hipStream_t s) {
+    NormArgs<CAP> a;
+    a.piece = piece;
     a.sums = static_cast<double *>(ws);
     a.norm = norm;
     a.max_norm = max_norm;
@@ -176,7 +174,7 @@ hipError_t launch_grad_norm(int count, const void *const *grads, const long *siz
             a.count = 0;
             a.base = base;
             int n = 0;
-            for (; i < count && a.count < kPerLaunch; ++i) {
+            for (; i < count && a.count < CAP; ++i) {
                 if (sizes[i] == 0) continue;
                 const int k = a.count++;
                 a.in[k] = grads[i];
@@ -184,15 +182,28 @@ hipError_t launch_grad_norm(int count, const void *const *grads, const long *siz
                 a.size[k] = sizes[i];
                 a.dtype[k] = (unsigned char)dtypes[i];
                 a.first[k] = n;
-                n += (int)((sizes[i] + a.piece - 1) / a.piece);
+                n += (int)((sizes[i] + piece - 1) / piece);
             }
             a.first[a.count] = n;
             if (!a.count) break;
-            if (clip) hipLaunchKernelGGL(clip_kernel, dim3(n), dim3(kThreads), 0, s, a);
-            else hipLaunchKernelGGL(norm_kernel, dim3(n), dim3(kThreads), 0, s, a);
+            if (clip) hipLaunchKernelGGL(clip_kernel<CAP>, dim3(n), dim3(kThreads), 0, s, a);
+            else hipLaunchKernelGGL(norm_kernel<CAP>, dim3(n), dim3(kThreads), 0, s, a);
             base += n;
         }
     }
+}
+
+}  // namespace
+
+size_t grad_norm_bytes(int count, const long *sizes) {
+    return up((size_t)pieces_of(count, sizes, piece_length(count, sizes)) * sizeof(double), 256);
+}
+
+hipError_t launch_grad_norm(int count, const void *const *grads, const long *sizes, const int *dtypes, void *const *out,
+                            float max_norm, float *norm, void *ws, hipStream_t s) {
+    const long piece = piece_length(count, sizes), pieces = pieces_of(count, sizes, piece);
+    if (count <= kFew) launch<kFew>(count, grads, sizes, dtypes, out, max_norm, norm, ws, piece, pieces, s);
+    else launch<kPerLaunch>(count, grads, sizes, dtypes, out, max_norm, norm, ws, piece, pieces, s);
     if (!out || !pieces)
         hipLaunchKernelGGL(norm_end_kernel, dim3(1), dim3(kThreads), 0, s, static_cast<const double *>(ws), (int)pieces, norm);
     return hipGetLastError();

@@ -43,12 +43,13 @@ def test_no_workspace_for_sizes_that_are_refused(dtype, N, D, V, T):
 
 
 def test_workspaces_hold_what_the_calls_keep():
-    """Lower bounds: two lists of keys and positions; the packed rows, and in fp32 the three terms of both operands."""
+    """Lower bounds: two lists of keys and positions; the packed rows, and in fp32 the terms of both
+    operands, two for the scores and three more for the gradients."""
     lib = pkg.load_library()
     assert lib.fftconv_embedding_workspace_bytes(1, 1000, 64, 5000, 0) >= 1000 * 16
     assert lib.fftconv_xent_workspace_bytes(pkg.FPROP, 1, 1000, 64, 5000) >= 1000 * 64 * 2
-    assert lib.fftconv_xent_workspace_bytes(pkg.FPROP, 0, 1000, 64, 5000) >= (1000 + 5000) * 64 * 6
-    assert lib.fftconv_xent_workspace_bytes(pkg.BPROP, 0, 1000, 64, 5000) >= (1000 + 5000) * 64 * 6 + 1000 * 64 * 4
+    assert lib.fftconv_xent_workspace_bytes(pkg.FPROP, 0, 1000, 64, 5000) >= (1000 + 5000) * 64 * 4
+    assert lib.fftconv_xent_workspace_bytes(pkg.BPROP, 0, 1000, 64, 5000) >= (1000 + 5000) * 64 * 10 + 1000 * 64 * 4
     assert lib.fftconv_xent_workspace_bytes(pkg.ACCGRAD, 0, 1000, 64, 5000) == 0
     # without the scores: a piece of them stays far below all of them
     assert lib.fftconv_xent_workspace_bytes(pkg.BPROP, 1, 16384, 64, 1 << 20) < 16384 * 2 * (1 << 20) // 8
