@@ -12,9 +12,9 @@
 // chunk is written straight to the table; what a chunk holds of a run that crosses its borders goes to the
 // workspace in fp32, and a second launch joins those parts, again in order.  So a token that half
 // of the text consists of costs what any other rows cost, and two calls give the same bits.
-// 16384 rows of 1024 bf16 features into a table of 32000: 53 us, of which sorting 18, the sums (99 MB read and
-// written, 21 us at a copy's rate) 26, joining 12.  What is over the floor are six launches and their chains of
-// dependent reads.
+// 16384 rows of 1024 bf16 features into a table of 32000: 52 us, of which sorting and clearing the table 23, the
+// sums 17, joining 12; the 99 MB that have to move are 21 us at a copy's rate.  What is over that are six launches
+// and their chains of dependent reads.
 #include "operands.hpp"
 
 namespace fc {
@@ -126,6 +126,8 @@ __global__ __launch_bounds__(kThreads) void planes_to_rows_kernel(TurnArgs<T> a)
 // ---------------------------------------------------------------------------------- sort
 // Least significant digit first, stable.  A block's waves take neighbouring stretches of its items, 64 at a
 // time; among those a lane's rank is the number of lower lanes with its digit, found by a ballot for each bit.
+// The launches are short of work for the chip: blocks behind the sorting ones write the table's zeros meanwhile
+// (a 32000x1024 bf16 table: 4 us more in four launches, 9 less in the sums').
 //  - Up to 4096 items one block sorts them in LDS, all digits in one launch (500 items: 5 us; 16384 of them
 //    would take 42, beside 21 for the launches of the other way).
 //  - More are sorted by blocks of 1024 with two launches a digit: counts by block, then places.  Where a
@@ -133,7 +135,7 @@ __global__ __launch_bounds__(kThreads) void planes_to_rows_kernel(TurnArgs<T> a)
 //    beyond that a launch turns counts into places.
 constexpr int kSortThreads = 1024, kSortWaves = 16;
 constexpr int kDigitBits = 8, kDigits = 1 << kDigitBits;
-constexpr int kOneBlock = 4096, kOneBlockClasses = 1 << 20;      // (which also clears a byte per class)
+constexpr int kOneBlock = 4096;
 constexpr int kItems = kSortThreads, kInline = 32;
 
 struct SortPlan {
@@ -145,9 +147,8 @@ SortPlan sort_plan(long N, int V) {
     int bits = 1;
     while (bits < 31 && (1L << bits) < V) ++bits;
     SortPlan p;
-    p.one = N <= kOneBlock && V <= kOneBlockClasses;
+    p.one = N <= kOneBlock;
     p.passes = (bits + kDigitBits - 1) / kDigitBits;
-    if (p.passes < 2 && !p.one) p.passes = 2;      // the first clears what the last one sets (`present`)
     p.bits = (bits + p.passes - 1) / p.passes;
     p.blocks = (int)((N + kItems - 1) / kItems);
     return p;
@@ -159,20 +160,27 @@ struct SortArgs {
     int *key_out, *idx_out;
     int *hist, *totals;       // [blocks][digits] and [digits]: counts, or places where there are totals
     int *count;               // how many rows have a token
-    unsigned char *present;   // [V], cleared by the first launch, set by the last; null where nobody asks
+    char *zero_from, *zero_to;    // what this launch's other blocks clear
     long N;
-    int V, shift, bits, passes, blocks;
-    int first, last, placed;
+    int shift, bits, passes, blocks;
+    int first, placed;
 };
 
 __device__ __forceinline__ int sort_key(const SortArgs &a, long at, long n) {
     return at < n ? a.first ? a.tok(at) : a.key_in[at] : -1;
 }
-__device__ __forceinline__ void clear_present(const SortArgs &a) {      // (its length is a multiple of 16)
-    uint4 *const p = reinterpret_cast<uint4 *>(a.present);
-    if (a.first && p)
-        for (long v = (long)blockIdx.x * kSortThreads + threadIdx.x; v < (a.V + 15) / 16; v += (long)gridDim.x * kSortThreads)
-            p[v] = make_uint4(0, 0, 0, 0);
+// The work of the blocks behind the sorting ones: kZeroBytes each.
+constexpr int kZeroBytes = kSortThreads * 16 * 4;
+__device__ __forceinline__ void write_zeros(const SortArgs &a, int block) {
+    char *const from = a.zero_from + (size_t)block * kZeroBytes;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        char *const p = from + (i * kSortThreads + threadIdx.x) * 16;
+        if (p + 16 <= a.zero_to) __builtin_memcpy(p, &zero, 16);
+        else
+            for (char *q = p; q < a.zero_to; q += 2) *reinterpret_cast<unsigned short *>(q) = 0;
+    }
 }
 
 // Rank of each of a lane's items among its wave's with the same digit; `mine` (the wave's counts by digit, zero
@@ -232,6 +240,7 @@ __device__ __forceinline__ void places_of(int *counts, int digit, int at) {
 
 template <int R>
 __global__ __launch_bounds__(kSortThreads) void sort_block_kernel(SortArgs a) {
+    if (blockIdx.x > 0) return write_zeros(a, blockIdx.x - 1);
     __shared__ int keys[R * kSortThreads];
     __shared__ unsigned short rows[R * kSortThreads];
     __shared__ int counts[kSortWaves * kDigits];
@@ -243,7 +252,6 @@ __global__ __launch_bounds__(kSortThreads) void sort_block_kernel(SortArgs a) {
         row[i] = begin + i * 64;
         key[i] = sort_key(a, row[i], a.N);
     }
-    clear_present(a);
     int n = 0;
     for (int p = 0; p < a.passes; ++p) {
         const int shift = p * a.bits;
@@ -278,7 +286,6 @@ __global__ __launch_bounds__(kSortThreads) void sort_block_kernel(SortArgs a) {
         if (key[i] >= 0) {
             a.key_out[begin + i * 64] = key[i];
             a.idx_out[begin + i * 64] = row[i];
-            if (a.present) a.present[key[i]] = 1;
         }
     if (tid == 0) *a.count = n;
 }
@@ -286,10 +293,10 @@ __global__ __launch_bounds__(kSortThreads) void sort_block_kernel(SortArgs a) {
 // Text is made of few tokens: the digit of the first lane that has one is counted by all lanes at once, the
 // others by an atomic each.
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortArgs a) {
+    if ((int)blockIdx.x >= a.blocks) return write_zeros(a, blockIdx.x - a.blocks);
     __shared__ int h[kDigits];
     const int nd = 1 << a.bits, tid = threadIdx.x;
     if (tid < nd) h[tid] = 0;
-    clear_present(a);
     __syncthreads();
     const long begin = (long)blockIdx.x * kItems, n = a.first ? a.N : (long)*a.count;
     const int key = sort_key(a, begin + tid, n), digit = (key >> a.shift) & (nd - 1);
@@ -329,6 +336,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_columns_kernel(SortArgs a) 
 }
 
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a) {
+    if ((int)blockIdx.x >= a.blocks) return write_zeros(a, blockIdx.x - a.blocks);
     __shared__ int counts[kSortWaves * kDigits];
     __shared__ int part[kSortWaves];
     const int nd = 1 << a.bits, tid = threadIdx.x, w = tid >> 6;
@@ -362,7 +370,6 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a) {
         const int to = counts[w * kDigits + ((key[0] >> a.shift) & (nd - 1))] + rank[0];
         a.key_out[to] = key[0];
         a.idx_out[to] = row;
-        if (a.last && a.present) a.present[key[0]] = 1;
     }
 }
 
@@ -374,15 +381,12 @@ struct SumArgs {
     const T *gy;
     const int *key, *idx;     // sorted
     const int *count;
-    const unsigned char *present;
     T *gtable;
     float *head, *tail;       // [chunks][D]: a chunk's part of the run that began before it / that goes on after it
     long chunks;
-    int D, V, C;              // C: sorted positions per chunk
+    int D, C;                 // C: sorted positions per chunk
     int lanes;                // threads of one row: a power of two, 8 elements each
     int slices;               // pieces of 8 * lanes elements in a row
-    long sum_blocks;          // the blocks behind these write zeros to the rows no token names
-    int zero_rows;            // rows per such block
     float scale;
     int accumulate;
 };
@@ -405,16 +409,6 @@ __device__ __forceinline__ void finish_row(const SumArgs<T> &a, int key, int d, 
 template <class T>
 __global__ __launch_bounds__(kThreads) void embedding_sum_kernel(SumArgs<T> a) {
     const int tid = threadIdx.x;
-    if ((long)blockIdx.x >= a.sum_blocks) {
-        const long v0 = ((long)blockIdx.x - a.sum_blocks) * a.zero_rows;
-        const int cpr = (a.D + 7) / 8;
-        const float zero[8] = {};
-        for (int c = tid; c < a.zero_rows * cpr; c += kThreads) {
-            const int r = c / cpr, d = (c - r * cpr) * 8;
-            if (v0 + r < a.V && !a.present[v0 + r]) store8(a.gtable + (size_t)(v0 + r) * a.D + d, a.D - d, zero);
-        }
-        return;
-    }
     // the chunk's tokens and rows first, so that its rows can be asked for at once
     __shared__ int keys[kThreads * kMostChunk / 8], rows[kThreads * kMostChunk / 8];
     const int groups = kThreads / a.lanes, g = tid / a.lanes, l = tid % a.lanes;
@@ -517,7 +511,7 @@ struct GradPlan {
     SortPlan sort;
     int lanes, slices, C;
     long chunks;
-    size_t rows, key[2], idx[2], hist, totals, count, present, head, tail, total;
+    size_t rows, key[2], idx[2], hist, totals, count, head, tail, total;
 };
 GradPlan grad_plan(int dtype, long N, int D, int V, int T) {
     GradPlan p;
@@ -538,7 +532,6 @@ GradPlan grad_plan(int dtype, long N, int D, int V, int T) {
     p.hist = take(p.sort.one ? 0 : (size_t)p.sort.blocks * (4u << p.sort.bits));
     p.totals = take(4u << p.sort.bits);
     p.count = take(4);
-    p.present = take((size_t)V + 15);
     p.head = take((size_t)p.chunks * D * 4);
     p.tail = take((size_t)p.chunks * D * 4);
     p.total = at;
@@ -549,11 +542,6 @@ long sum_blocks(const GradPlan &p) {
     const long groups = kThreads / p.lanes;
     return (p.chunks * p.slices + groups - 1) / groups;
 }
-int zero_rows(int D) {
-    const int rows = 1024 / ((D + 7) / 8);
-    return rows < 1 ? 1 : rows > 64 ? 64 : rows;
-}
-
 template <class T>
 hipError_t fprop(const void *table, Tokens tok, void *y, long N, int D, int Tn, float scale, hipStream_t s) {
     if (Tn) {
@@ -586,40 +574,47 @@ hipError_t accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, 
     so.tok = tok;
     so.count = reinterpret_cast<int *>(ws + p.count);
     so.hist = reinterpret_cast<int *>(ws + p.hist); so.totals = reinterpret_cast<int *>(ws + p.totals);
-    so.present = accumulate ? nullptr : reinterpret_cast<unsigned char *>(ws + p.present);
-    so.N = N; so.V = V; so.bits = p.sort.bits; so.passes = p.sort.passes; so.blocks = p.sort.blocks;
+    so.N = N; so.bits = p.sort.bits; so.passes = p.sort.passes; so.blocks = p.sort.blocks;
     so.placed = p.sort.blocks > kInline;
     so.key_out = reinterpret_cast<int *>(ws + p.key[0]);
     so.idx_out = reinterpret_cast<int *>(ws + p.idx[0]);
+    // the table's bytes, in as many parts as launches clear them
+    char *const begin = static_cast<char *>(gtable);
+    const size_t bytes = accumulate ? 0 : (size_t)V * D * sizeof(T), launches = p.sort.one ? 1 : 2 * p.sort.passes;
+    const auto clear = [&](size_t i) {
+        so.zero_from = begin + bytes / 16 * i / launches * 16;
+        so.zero_to = i + 1 == launches ? begin + bytes : begin + bytes / 16 * (i + 1) / launches * 16;
+        return (unsigned)((so.zero_to - so.zero_from + kZeroBytes - 1) / kZeroBytes);
+    };
     if (p.sort.one) {
         so.first = 1;
-        if (N <= 1024) hipLaunchKernelGGL(sort_block_kernel<1>, dim3(1), dim3(kSortThreads), 0, s, so);
-        else hipLaunchKernelGGL(sort_block_kernel<4>, dim3(1), dim3(kSortThreads), 0, s, so);
+        const unsigned grid = 1 + clear(0);
+        if (N <= 1024) hipLaunchKernelGGL(sort_block_kernel<1>, dim3(grid), dim3(kSortThreads), 0, s, so);
+        else hipLaunchKernelGGL(sort_block_kernel<4>, dim3(grid), dim3(kSortThreads), 0, s, so);
     } else {
         for (int i = 0; i < p.sort.passes; ++i) {
-            so.first = i == 0; so.last = i + 1 == p.sort.passes;
+            so.first = i == 0;
             so.shift = i * p.sort.bits;
             so.key_in = reinterpret_cast<int *>(ws + p.key[(i + 1) & 1]);
             so.idx_in = reinterpret_cast<int *>(ws + p.idx[(i + 1) & 1]);
             so.key_out = reinterpret_cast<int *>(ws + p.key[i & 1]);
             so.idx_out = reinterpret_cast<int *>(ws + p.idx[i & 1]);
-            hipLaunchKernelGGL(sort_count_kernel, dim3(so.blocks), dim3(kSortThreads), 0, s, so);
+            unsigned grid = so.blocks + clear(2 * i);
+            hipLaunchKernelGGL(sort_count_kernel, dim3(grid), dim3(kSortThreads), 0, s, so);
             if (so.placed) hipLaunchKernelGGL(sort_columns_kernel, dim3(((1 << so.bits) + 63) / 64), dim3(kSortThreads), 0, s, so);
-            hipLaunchKernelGGL(sort_place_kernel, dim3(so.blocks), dim3(kSortThreads), 0, s, so);
+            grid = so.blocks + clear(2 * i + 1);
+            hipLaunchKernelGGL(sort_place_kernel, dim3(grid), dim3(kSortThreads), 0, s, so);
         }
     }
     SumArgs<T> a{};
     a.gy = rows;
-    a.key = so.key_out; a.idx = so.idx_out; a.count = so.count; a.present = so.present;
+    a.key = so.key_out; a.idx = so.idx_out; a.count = so.count;
     a.gtable = static_cast<T *>(gtable);
     a.head = reinterpret_cast<float *>(ws + p.head);
     a.tail = reinterpret_cast<float *>(ws + p.tail);
-    a.chunks = p.chunks; a.D = D; a.V = V; a.C = p.C; a.lanes = p.lanes; a.slices = p.slices;
+    a.chunks = p.chunks; a.D = D; a.C = p.C; a.lanes = p.lanes; a.slices = p.slices;
     a.scale = scale; a.accumulate = accumulate;
-    a.sum_blocks = sum_blocks(p);
-    a.zero_rows = zero_rows(D);
-    const long zero_blocks = accumulate ? 0 : ((long)V + a.zero_rows - 1) / a.zero_rows;
-    hipLaunchKernelGGL(embedding_sum_kernel<T>, dim3((unsigned)(a.sum_blocks + zero_blocks)), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(embedding_sum_kernel<T>, dim3((unsigned)sum_blocks(p)), dim3(kThreads), 0, s, a);
     if (p.chunks > 1) hipLaunchKernelGGL(embedding_join_kernel<T>, dim3((unsigned)p.chunks), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
@@ -633,7 +628,7 @@ bool embedding_fits(bool accgrad, long N, int D, int V, int T) {
     if (T && (double)N / T * ((T + 63) / 64) * ((D + 63) / 64) > 0x7fffffff) return false;
     if (!accgrad) return true;
     const GradPlan p = grad_plan(kF32, N, D, V, T);
-    return p.chunks <= 0x7fffffff && (double)sum_blocks(p) + ((double)V / zero_rows(D) + 1) <= 0x7fffffff;
+    return p.chunks <= 0x7fffffff && sum_blocks(p) <= 0x7fffffff && (double)V * D * 4 / kZeroBytes + p.sort.blocks + 1 <= 0x7fffffff;
 }
 
 hipError_t launch_embedding_fprop(int dtype, const void *table, Tokens tok, void *y, long N, int D, int T, float scale, hipStream_t s) {

@@ -88,6 +88,8 @@ __host__ __device__ inline int rows_splits(long tiles, int places, int most) {
     return (int)(s < 1 ? 1 : s > most ? most : s);
 }
 
+// Loads from memory to LDS, in lane order from m0 on.  As assembly, so that an LDS read waits for the step that it
+// needs (landed_and_met) and not for all that is on its way; no register is written.
 __device__ __forceinline__ void lds_load16(const char *from, unsigned lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
 }
