@@ -386,8 +386,9 @@ const char *fftconv_last_kernel_label(fftconv_handle h, int i);
  *    that a gradient which is not accumulated becomes zero.
  *  - Results do not depend on the order in which workgroups run: the same call gives the same bits.
  *  - The calls run on the handle's device, whichever is current.  `ws`: 16-byte aligned device scratch
- *    of at least the size function's bytes, or NULL for the handle's own buffer.  Under graph capture a
- *    workspace must be passed (else FFTCONV_WORKSPACE_TOO_SMALL): the handle's buffer may move later.
+ *    of at least the size function's bytes, or NULL for a buffer of the handle's (not the one of the passes, which a
+ *    captured pass may hold), grown as theirs is.  Under graph capture a workspace must be passed (else
+ *    FFTCONV_WORKSPACE_TOO_SMALL): the handle's buffer may move later.
  *    Two graphs that may run at the same time need two workspaces.
  */
 enum { FFTCONV_F32 = 0, FFTCONV_BF16 = 1, FFTCONV_F16 = 2 };

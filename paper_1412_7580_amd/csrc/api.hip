@@ -283,7 +283,7 @@ int fc::hip_fail(fftconv_ctx *c, hipError_t e) {
     return FFTCONV_HIP_ERROR;
 }
 
-int fc::get_workspace(fftconv_ctx *c, size_t need, void **ws, size_t ws_bytes) {
+static int get_workspace(fftconv_ctx *c, size_t need, void **ws, size_t ws_bytes) {
     if (*ws) return ws_bytes < need ? FFTCONV_WORKSPACE_TOO_SMALL : FFTCONV_OK;
     hipError_t e;
     if (c->ws_bytes < need) {
@@ -523,6 +523,7 @@ int fftconv_create(fftconv_handle *out, int device) {
     fftconv_ctx *c = new (std::nothrow) fftconv_ctx();
     if (!c) return FFTCONV_HIP_ERROR;
     c->device = device; c->stream = nullptr; c->ws = nullptr; c->ws_bytes = 0;
+    c->step_ws = nullptr; c->step_ws_bytes = 0;
     c->profiling = 0; c->nk = 0; c->last_hip_error[0] = 0;
     c->static_scratch = nullptr;
     c->sw = read_gemm_switches();
@@ -542,6 +543,7 @@ int fftconv_create(fftconv_handle *out, int device) {
 int fftconv_destroy(fftconv_handle h) {
     if (!h) return FFTCONV_INVALID_ARG;
     if (h->ws) (void)hipFree(h->ws);
+    if (h->step_ws) (void)hipFree(h->step_ws);
     for (int i = 0; i < 2 * kMaxKernels; ++i) (void)hipEventDestroy(h->ev[i]);
     delete h->plans;
     delete h;

@@ -13,6 +13,8 @@ struct fftconv_ctx {
     hipStream_t stream;
     void *ws;
     size_t ws_bytes;
+    void *step_ws;          // of the operators around the passes: a captured pass may hold `ws`, which they must not move
+    size_t step_ws_bytes;
     void *static_scratch;   // this device's copy of fftconv_static_scratch (device address)
     int profiling;
     hipEvent_t ev[2 * kMaxKernels];   // start/stop pair per kernel of the last call
@@ -25,7 +27,4 @@ namespace fc {
 
 // Keeps the HIP error's text in the handle and returns FFTCONV_HIP_ERROR.
 int hip_fail(fftconv_ctx *c, hipError_t e);
-// *ws of at least `need` bytes: the caller's, or the handle's own, grown where it is too short.
-int get_workspace(fftconv_ctx *c, size_t need, void **ws, size_t ws_bytes);
-
 }  // namespace fc

@@ -36,8 +36,8 @@ int check_sizes(int dtype, int token_bits, long N, int D, int V, int T) {
     return FFTCONV_OK;
 }
 
-// The workspace of a call: the caller's, or the handle's.  A captured call keeps the address it was
-// given for as long as its graph lives, and the handle's buffer moves when a later call needs more:
+// The workspace of a call: the caller's, or the handle's buffer for these operators.  A captured call keeps the
+// address it was given for as long as its graph lives, and that buffer moves when a later call needs more:
 // under capture only the caller's will do.
 int workspace(fftconv_ctx *c, size_t need, void **ws, size_t bytes) {
     if (*ws) {
@@ -46,7 +46,18 @@ int workspace(fftconv_ctx *c, size_t need, void **ws, size_t bytes) {
     }
     hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
     if (hipStreamIsCapturing(c->stream, &cap) == hipSuccess && cap != hipStreamCaptureStatusNone) return FFTCONV_WORKSPACE_TOO_SMALL;
-    return get_workspace(c, need, ws, 0);
+    if (c->step_ws_bytes < need) {
+        hipError_t e;
+        if (c->step_ws) {
+            if ((e = hipStreamSynchronize(c->stream)) != hipSuccess) return hip_fail(c, e);
+            (void)hipFree(c->step_ws);
+            c->step_ws = nullptr; c->step_ws_bytes = 0;
+        }
+        if ((e = hipMalloc(&c->step_ws, need)) != hipSuccess) return hip_fail(c, e);
+        c->step_ws_bytes = need;
+    }
+    *ws = c->step_ws;
+    return FFTCONV_OK;
 }
 
 int done(fftconv_ctx *c, hipError_t e) { return e == hipSuccess ? FFTCONV_OK : hip_fail(c, e); }

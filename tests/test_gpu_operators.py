@@ -384,6 +384,32 @@ def test_capture_without_an_eager_call_before(lib):
         h.close()
 
 
+def test_a_captured_pass_keeps_its_buffer(lib):
+    """A convolution pass captured on the handle's own buffer: operators that need more than that buffer holds run
+    between the replays and leave it where it is."""
+    h = lib.Handle(0)
+    try:
+        g = gen(53)
+        x, w = torch.randn(8, 8, 13, 13, generator=g, device="cuda"), torch.randn(8, 8, 3, 3, generator=g, device="cuda")
+        want = h.fft_conv_fprop(x, w).clone()
+        y = torch.empty_like(want)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            h.fft_conv_fprop(x, w, y=y)
+        for n in (300, 3000):
+            f, c = torch.randn(n, 64, generator=g, device="cuda"), torch.randn(9000, 64, generator=g, device="cuda")
+            t = tokens_for(g, (n,), 9000)
+            _, lse = h.xent_fprop(f, c, t)
+            h.xent_backward(f, c, t, lse)
+            h.embedding_accgrad(f, t, 9000)
+            y.fill_(7)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(y, want)
+    finally:
+        h.close()
+
+
 @pytest.mark.parametrize("seed", range(30))
 def test_random_sizes(hd, seed):
     import random
