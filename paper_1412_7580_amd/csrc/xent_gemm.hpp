@@ -71,6 +71,7 @@ struct GemmArgs {
     const float *lse, *coef; // by row
     int n0;                  // class of column 0
     void *G;                 // (from two terms: in three)
+    int twice;               // (small tiles) rows come in pairs: an odd one holds what the rounding of the even one's G left
     long g_ld, g_term;
     long part_ld;
     // rows, classes
@@ -478,6 +479,12 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
                         if constexpr (GT == 3) {
                             split4(g[0], g[1], g[2], g[3], t[0][h], t[1][h], t[2][h]);
                         } else {
+                            if (BM == 128 && a.twice && (lm & 1))
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) {
+                                    const float held = (float)(T)g[r];
+                                    g[r] = fabsf(held) < INFINITY ? g[r] - held : 0.f;
+                                }
                             T v[4] = {(T)g[0], (T)g[1], (T)g[2], (T)g[3]};
                             __builtin_memcpy(&t[0][h], v, 8);
                         }

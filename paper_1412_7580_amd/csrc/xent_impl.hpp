@@ -21,7 +21,7 @@
 // lies behind the count ends at once.
 //
 // G is held in the operands' type (fp32: in three terms): one rounding of each element, half a step
-// of its own size, beside the one rounding of the gradients.  fp16 holds it times a power of two
+// of its own size, beside the one rounding of the gradients; a few rows bring what it left as well.  fp16 holds it times a power of two
 // that lifts the largest dL/dloss to 2^13 .. 2^14: what underflows is below 2^-37 of it.
 #pragma once
 #include "xent_gemm.hpp"
@@ -53,6 +53,7 @@ struct ScanArgs {
     float *lse_out, *coef, *alpha;
     float scale;
     int mean, half_range;           // half_range: G is held in fp16
+    int copies;                     // packed rows to a row
 };
 
 struct ScanRows { int t[4], mine, upto; float top; };
@@ -139,13 +140,15 @@ __global__ __launch_bounds__(kThreads) void xent_place_kernel(ScanArgs a) {
         const long n = n0 + tid * 4 + e;
         if (n >= a.N) break;
         const bool has = r.t[e] >= 0;
-        if (a.pos) a.pos[n] = has ? at : -1;
+        if (a.pos) a.pos[n] = has ? at * a.copies : -1;
         if (has) {
-            a.row_of[at] = (int)n;
-            a.target[at] = r.t[e];
-            if (a.coef) {
-                a.lse_out[at] = a.lse_in[n];
-                a.coef[at] = (a.gloss ? a.gloss[n] : 1.f) * up;
+            for (int q = at * a.copies; q < (at + 1) * a.copies; ++q) {
+                a.row_of[q] = (int)n;
+                a.target[q] = r.t[e];
+                if (a.coef) {
+                    a.lse_out[q] = a.lse_in[n];
+                    a.coef[q] = (a.gloss ? a.gloss[n] : 1.f) * up;
+                }
             }
             ++at;
         } else if (a.loss) {
@@ -154,7 +157,7 @@ __global__ __launch_bounds__(kThreads) void xent_place_kernel(ScanArgs a) {
         }
     }
     if (blockIdx.x == 0 && tid == 0) {
-        *a.count = total;
+        *a.count = total * a.copies;
         *a.zeros = make_uint4(0, 0, 0, 0);
         if (a.alpha) *a.alpha = total ? ldexpf(a.mean ? a.scale / (float)total : a.scale, -e2) : 0.f;
     }
@@ -348,6 +351,7 @@ struct RowsOutArgs {
     S *gx;
     long N, ld;
     int bm, tiles_n, places, most, D, T_;
+    int copies;               // rows of partial to a row
 };
 
 // The sum of parts from, from + 1, ... below to, eight of them asked for at a time.
@@ -369,6 +373,16 @@ __device__ __forceinline__ void sum_parts(const float *p, size_t stride, int fro
 }
 
 struct RowParts { int splits; size_t stride; };
+// Parts from, ... below to, of packed row `at` and of what the rounding of its G left.
+template <class S>
+__device__ __forceinline__ void sum_row(const RowsOutArgs<S> &a, const RowParts &parts, int at, int d, int from, int to, float (&f)[8]) {
+    sum_parts(a.partial + (size_t)at * a.ld + d, parts.stride, from, to, a.D - d, f);
+    if (a.copies == 1) return;
+    float rest[8];
+    sum_parts(a.partial + (size_t)(at + 1) * a.ld + d, parts.stride, from, to, a.D - d, rest);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] += rest[i];
+}
 template <class S>
 __device__ __forceinline__ RowParts parts_of(const RowsOutArgs<S> &a) {
     const int tiles_m = (*a.count + a.bm - 1) / a.bm;
@@ -390,7 +404,7 @@ __global__ __launch_bounds__(kThreads) void xent_rows_out_kernel(RowsOutArgs<S> 
         const long n = (long)(c / cpr);
         const int d = (int)(c - (size_t)n * cpr) * 8, at = c < total ? a.pos[n] : -1;
         float f[8] = {};
-        if (at >= 0) sum_parts(a.partial + (size_t)at * a.ld + d, parts.stride, from, to, a.D - d, f);
+        if (at >= 0) sum_row(a, parts, at, d, from, to, f);
         if constexpr (G > 1) {
             __syncthreads();
 #pragma unroll
@@ -420,7 +434,7 @@ __global__ __launch_bounds__(kThreads) void xent_planes_out_kernel(RowsOutArgs<S
         float f[8] = {};
         if (t0 + q < a.T_ && d0 + dd < a.D) {
             const int at = a.pos[(long)s * a.T_ + t0 + q];
-            if (at >= 0) sum_parts(a.partial + (size_t)at * a.ld + d0 + dd, parts.stride, 0, parts.splits, a.D - d0 - dd, f);
+            if (at >= 0) sum_row(a, parts, at, d0 + dd, 0, parts.splits, f);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) tile[dd + i][q] = f[i] * alpha;
@@ -669,14 +683,14 @@ inline long places(const Shape &s) { return s.bm == 256 ? kBigPlaces : kSmallPla
 // Where the reduction may be split, it is, until there is a block for every place; such products take
 // tiles 192 columns wide where that covers the columns with less (384 columns: 97 -> 75 us for 15488 rows
 // and 1000 classes in fp32).
-inline Shape shape_of(long M, long N, long K, int terms, bool split) {
+inline Shape shape_of(long M, long N, long K, int terms, bool split, bool small = false) {
     const long steps = (K + kStep - 1) / kStep, parts = steps * (terms == 3 ? 6 : 1) / 6;      // of six products at least
     Shape s{};
     s.most = split ? (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts) : 1;
     const auto tiles = [](long n, long t) { return (n + t - 1) / t; };
     s.bm = 256;
     s.bn = split && tiles(N, 192) * 192 < tiles(N, 256) * 256 ? 192 : 256;
-    if (tiles(M, s.bm) * tiles(N, s.bn) * s.most < 192) s.bm = s.bn = 128;
+    if (small || tiles(M, s.bm) * tiles(N, s.bn) * s.most < 192) s.bm = s.bn = 128;
     s.tiles_m = (int)tiles(M, s.bm);
     s.tiles_n = (int)tiles(N, s.bn);
     s.splits = rows_splits((long)s.tiles_m * s.tiles_n, (int)places(s), s.most);
@@ -684,7 +698,8 @@ inline Shape shape_of(long M, long N, long K, int terms, bool split) {
 }
 
 struct XentPlan {
-    long Np;                  // rows, up to a multiple of 256
+    int copies;               // packed rows to a row
+    long R, Np;               // packed rows at most, and up to a multiple of 256
     int Dp, Dc;               // features, up to a multiple of 8 and of 4
     int terms;                // of fp32 in the gradients' products
     bool pack_w;
@@ -719,9 +734,18 @@ inline void thin_plan(XentPlan &p, int dtype, long N, int D, int V) {
 // holds, cost 1 .. 11 % more than 640 (16384 rows of 768 features, 50257 classes: 4.44 ms and 3.99).
 constexpr size_t kPieceBytes = (size_t)640 << 20;
 
+// Gradients of up to so many rows of a 16-bit type take each row twice, the second time with what the rounding of
+// its G left.  Over more rows these roundings average out: 1.2 times the error of the results' own rounding.  Over
+// one to four a row's gradient is its target's coefficient times a vector, and that one rounding made it up to 2.6
+// times as far off.  All of them fit one tile of the products; a call takes 3 us more (8 rows of 1024 features,
+// 32000 classes: 81 and 85; of 256 features, 1000 classes: 32 and 35).
+constexpr long kPairedRows = 8;
+
 inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool aligned) {
     XentPlan p{};
-    p.Np = ceil_to(N, 256);
+    p.copies = backward && dtype != kF32 && N <= kPairedRows ? 2 : 1;
+    p.R = N * p.copies;
+    p.Np = ceil_to(p.R, 256);
     p.Dp = (int)ceil_to(D, 8);
     p.Dc = (int)ceil_to(D, 4);
     p.terms = dtype == kF32 ? 3 : 1;
@@ -735,7 +759,7 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
         p.total = at;
         return p;
     }
-    p.row_of = take((size_t)N * 4);
+    p.row_of = take((size_t)p.R * 4);
     p.target = take((size_t)p.Np * 4);                   // (the products read the rows' values a tile at a time)
     p.count = take(32);                                  // count, alpha, and from 16 on zeros
     p.scan_blocks = (int)((N + kScanRows - 1) / kScanRows);
@@ -762,9 +786,9 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
         p.piece = (int)ceil_to(((long)V + p.pieces - 1) / p.pieces, 256);
         p.pieces = (int)(((long)V + p.piece - 1) / p.piece);
         const long widest = p.piece < V ? p.piece : V;
-        p.score = shape_of(N, widest, D, p.terms, false);
-        p.rows = shape_of(N, D, widest, p.terms, true);
-        p.classes = shape_of(widest, D, N, p.terms, true);
+        p.score = shape_of(p.R, widest, D, p.terms, false, p.copies == 2);
+        p.rows = shape_of(p.R, D, widest, p.terms, true);
+        p.classes = shape_of(widest, D, p.R, p.terms, true);
         p.G = take((size_t)p.Np * p.terms * ceil_to(widest, 64) * 2);
         // the rows product splits by the tiles of rows that have a target: the fewer, the more parts, but never more
         // tiles in all than places, or than one part of all rows
@@ -830,7 +854,7 @@ struct Xent {
     const void *zeros() const { return ws + p.count + 16; }
 
     void scan(ScanArgs &sc) {
-        sc.tok = c.tok; sc.N = c.N; sc.blocks = p.scan_blocks;
+        sc.tok = c.tok; sc.N = c.N; sc.blocks = p.scan_blocks; sc.copies = p.copies;
         sc.counts = at<int>(p.counts); sc.tops = at<float>(p.tops);
         sc.row_of = at<int>(p.row_of); sc.target = at<int>(p.target); sc.count = at<int>(p.count); sc.zeros = at<uint4>(p.count + 16);
         if (sc.blocks > kScanInline) hipLaunchKernelGGL(xent_count_kernel, dim3(sc.blocks), dim3(kThreads), 0, s, sc);
@@ -929,8 +953,8 @@ struct Xent {
             g.M = (int)p.Np; g.N = width; g.K = c.D;
             g.target = sc.target; g.lse = sc.lse_out; g.coef = sc.coef;
             g.n0 = (int)v0;
-            g.G = at<Grad>(p.G); g.g_ld = ld; g.g_term = ld;
-            if (hipError_t e = product<Score, kGrad, kScore>(g, tiles(p.score, c.N, width), s); e != hipSuccess) return e;
+            g.G = at<Grad>(p.G); g.g_ld = ld; g.g_term = ld; g.twice = p.copies == 2;
+            if (hipError_t e = product<Score, kGrad, kScore>(g, tiles(p.score, p.R, width), s); e != hipSuccess) return e;
             if (c.gx) {
                 GemmArgs r{};
                 r.P = G; r.Q = grad_weights(v0);
@@ -944,7 +968,7 @@ struct Xent {
                 GemmArgs w{};
                 w.P = G; w.Q = grad_features();
                 w.count = sc.count; w.zeros = zeros();
-                w.M = width; w.N = c.D; w.K = (int)c.N;
+                w.M = width; w.N = c.D; w.K = (int)p.R;
                 w.alpha_scale = sc.alpha;
                 S *gw = static_cast<S *>(c.gw) + v0 * c.D;
                 const Shape sh = tiles(p.classes, width, c.D);
@@ -959,7 +983,7 @@ struct Xent {
         }
         if (c.gx) {
             const RowsOutArgs<S> o{at<float>(p.gx), sc.pos, sc.count, sc.alpha, static_cast<S *>(c.gx), c.N, p.Dc,
-                                   p.rows.bm, p.rows.tiles_n, (int)places(p.rows), p.rows.most, c.D, c.T};
+                                   p.rows.bm, p.rows.tiles_n, (int)places(p.rows), p.rows.most, c.D, c.T, p.copies};
             if (c.T) {
                 const long blocks = c.N / c.T * ((c.T + 63) / 64) * ((c.D + 63) / 64);
                 hipLaunchKernelGGL(xent_planes_out_kernel<S>, dim3((unsigned)blocks), dim3(kThreads), 0, s, o);

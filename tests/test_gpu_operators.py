@@ -129,11 +129,12 @@ def test_embedding_beyond_32_bit_offsets(hd):
 
 
 # ---------------------------------------------------------------------------------- cross entropy
-def xent_reference(x, w, tokens, gloss, scale, mean, planes):
+def xent_reference(x, w, tokens, gloss, scale, mean, planes, kept=None):
     """Loss, lse, gx, gw and how far each may be off, in 64 bits."""
     dtype, V, D = x.dtype, w.shape[0], w.shape[1]
     u, tiny = half_step(dtype), TINY[dtype]
-    kept = 0.0 if dtype == torch.float32 else u              # fp32: G keeps three terms, all of it
+    if kept is None:
+        kept = 0.0 if dtype == torch.float32 else u          # fp32: G keeps three terms, all of it
     terms = 6 if dtype == torch.float32 else 1
     has, at = picks(tokens, V)
     X = torch.where(has[:, None], rows_of(x, planes).double(), torch.zeros((), device="cuda", dtype=torch.float64))
@@ -195,6 +196,39 @@ def test_xent(hd, shape, D, V, planes, dtype):
     want, bound = ref["gw"]
     want = want + w.double()
     within(acc, want, bound + 2 * E * want.abs() + half_step(dtype) * (want.abs() + bound), "gw, accumulated")
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:], ids=["bf16", "f16"])
+@pytest.mark.parametrize("N,T,D,V,mean", [(1, 0, 64, 20, True), (1, 0, 333, 1001, False), (2, 0, 1000, 20011, True), (4, 2, 40, 300, True), (8, 0, 8, 3, False), (8, 8, 256, 65536, True)])
+def test_xent_gradients_of_few_rows_have_one_rounding(hd, N, T, D, V, mean, dtype):
+    # What the rounding of a row's G leaves, at most half a step of it, is taken along, rounded itself: G is held
+    # to u^2.  (With one rounding of G, u, a gradient made of one coefficient is up to 2 u off.)
+    g = gen(N * 1000 + D)
+    tokens = torch.randint(0, V, (N // T, T) if T else (N,), generator=g, device="cuda")
+    if N > 2:
+        tokens.view(-1)[1] = -1
+    x = torch.randn((N // T, D, T) if T else (N, D), generator=g, device="cuda").to(dtype)
+    w = (torch.randn(V, D, generator=g, device="cuda") / math.sqrt(D)).to(dtype)
+    gloss = torch.randn(tokens.shape, generator=g, device="cuda")
+    ref = xent_reference(x, w, tokens, gloss, 1.0, mean, bool(T), kept=half_step(dtype) ** 2)
+    _, lse = hd.xent_fprop(x, w, tokens, planes=bool(T))
+    gx, gw = hd.xent_backward(x, w, tokens, lse, gloss=gloss, mean=mean, planes=bool(T))
+    within(rows_of(gx, bool(T)), *ref["gx"], "gx")
+    within(gw, *ref["gw"], "gw")
+    only_x, _ = hd.xent_backward(x, w, tokens, lse, gloss=gloss, mean=mean, planes=bool(T), want_gw=False)
+    _, only_w = hd.xent_backward(x, w, tokens, lse, gloss=gloss, mean=mean, planes=bool(T), want_gx=False)
+    assert torch.equal(gx, only_x) and torch.equal(gw, only_w)
+
+
+@pytest.mark.parametrize("N", [1, 8])
+def test_xent_gradients_of_few_rows_whose_loss_gradient_is_not_finite(hd, N):
+    # gw's row of a class: G x, where G is the product of an infinite dL/dloss and a probability: infinite with x's sign
+    x = torch.ones(N, 16, device="cuda", dtype=torch.bfloat16)
+    w = torch.zeros(4, 16, device="cuda", dtype=torch.bfloat16)
+    tokens = torch.zeros(N, device="cuda", dtype=torch.int64)
+    _, lse = hd.xent_fprop(x, w, tokens)
+    _, gw = hd.xent_backward(x, w, tokens, lse, gloss=torch.full((N,), math.inf, device="cuda"), want_gx=False)
+    assert torch.equal(gw[1:], torch.full((3, 16), math.inf, device="cuda", dtype=torch.bfloat16)) and bool((gw[0] == -math.inf).all())
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16", "f16"])
