@@ -13,7 +13,7 @@
 // 400 million bf16 elements: norm 178 us (4.5 TB/s), scaling 309 (1.6 GB, 5.2 TB/s: the last of what the norm read
 // comes from the cache); a copy runs at 4.8.
 //
-// A norm that is zero, infinite or not a number leaves the tensors as they are: the caller sees it in `norm`.
+// A norm that is zero, infinite in fp32 or not a number leaves the tensors as they are: the caller sees it in `norm`.
 #include "operands.hpp"
 
 namespace fc {
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(NormArgs<CAP> a) {
     __shared__ double lds[4];
     const double norm = sqrt(total(a.sums, a.pieces, lds));
     if (a.base == 0 && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
-    const bool clip = norm > (double)a.max_norm && norm < 1.7e308;
+    const bool clip = norm > (double)a.max_norm && (float)norm < INFINITY;
     const float c = clip ? (float)((double)a.max_norm / norm) : 1.f;
     const int p = (int)(gridDim.x - 1 - blockIdx.x), t = tensor_of(a, p);
     if (!clip && a.in[t] == a.out[t]) return;

@@ -543,6 +543,14 @@ def test_norms_that_say_nothing_leave_the_values(hd, value):
     assert torch.equal(t.nan_to_num(9.0), before.nan_to_num(9.0)) and torch.equal(out.nan_to_num(9.0), before.nan_to_num(9.0))
 
 
+@pytest.mark.parametrize("dtype", TYPES[:2], ids=["f32", "bf16"])
+def test_a_norm_beyond_fp32_is_infinite_and_leaves_the_values(hd, dtype):
+    t = torch.full((5000,), 3e38, device="cuda").to(dtype)
+    before, out = t.clone(), torch.empty_like(t)
+    assert math.isinf(float(hd.grad_norm([t]))) and math.isinf(float(hd.grad_clip([t], 1.0, out=[out]))) and math.isinf(float(hd.grad_clip([t], 1.0)))
+    assert torch.equal(t, before) and torch.equal(out, before)
+
+
 def test_an_empty_list_has_norm_zero(hd):
     assert float(hd.grad_norm([])) == 0 and float(hd.grad_clip([], 1.0)) == 0
     assert float(hd.grad_norm([torch.empty(0, device="cuda")])) == 0
