@@ -105,8 +105,10 @@ __global__ __launch_bounds__(kThreads) void norm_end_kernel(const double *sums, 
     if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
+// The factor is c * c2: one below fp32's normal range (2^-126) would lose bits that the results have.
+struct Factor { float c, c2; };
 template <class T>
-__device__ __forceinline__ void scaled(const T *in, T *out, long n, float c) {
+__device__ __forceinline__ void scaled(const T *in, T *out, long n, Factor k) {
     constexpr int U = 4;
     long i = (long)threadIdx.x * 8;
     for (; i + (U - 1) * kThreads * 8L + 8 <= n; i += U * kThreads * 8L) {
@@ -116,7 +118,7 @@ __device__ __forceinline__ void scaled(const T *in, T *out, long n, float c) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[u][j] *= c;
+            for (int j = 0; j < 8; ++j) f[u][j] = f[u][j] * k.c * k.c2;
             store8(out + i + u * kThreads * 8L, 8, f[u]);
         }
     }
@@ -125,7 +127,7 @@ __device__ __forceinline__ void scaled(const T *in, T *out, long n, float c) {
         float f[8];
         load8(in + i, m, f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] *= c;
+        for (int j = 0; j < 8; ++j) f[j] = f[j] * k.c * k.c2;
         store8(out + i, m, f);
     }
 }
@@ -137,7 +139,8 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(NormArgs<CAP> a) {
     const double norm = sqrt(total(a.sums, a.pieces, lds));
     if (a.base == 0 && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
     const bool clip = norm > (double)a.max_norm && (float)norm < INFINITY;
-    const float c = clip ? (float)((double)a.max_norm / norm) : 1.f;
+    const double whole = clip ? (double)a.max_norm / norm : 1.0;
+    const Factor c = whole < 0x1p-126 ? Factor{(float)(whole * 0x1p100), 0x1p-100f} : Factor{(float)whole, 1.f};
     const int p = (int)(gridDim.x - 1 - blockIdx.x), t = tensor_of(a, p);
     if (!clip && a.in[t] == a.out[t]) return;
     const long from = (long)(p - a.first[t]) * a.piece;

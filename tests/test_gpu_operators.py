@@ -532,6 +532,14 @@ def test_norm_where_squares_leave_fp32(hd):
     assert float((big - 0.5).abs().max()) <= 4 * E
 
 
+@pytest.mark.parametrize("value,max_norm", [(1e38, 1e-3), (1e30, 1e-15), (3e37, 1.0), (1e-10, 1e-37)])
+def test_clipping_by_any_factor(hd, value, max_norm):
+    # four equal elements of norm twice theirs: each becomes max_norm / 2, off by the roundings of two factors and products
+    t = torch.full((4,), value, device="cuda")
+    hd.grad_clip([t], max_norm)
+    assert float((t.double() - max_norm / 2).abs().max()) <= 5 * E * max_norm / 2 + 2.0 ** -150
+
+
 @pytest.mark.parametrize("value", [math.nan, math.inf, 0.0])
 def test_norms_that_say_nothing_leave_the_values(hd, value):
     t = torch.ones(5000, device="cuda") if value else torch.zeros(5000, device="cuda")
