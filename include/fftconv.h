@@ -408,8 +408,8 @@ int fftconv_embedding_accgrad(fftconv_handle hd, int dtype, const void *gy, cons
  * backward takes the lse that fprop left for the same x, wt and targets, and gives gx (x's shape) and gw[V, D]
  * of the loss  scale * sum_n gloss[n] loss[n]  (gloss NULL: all ones), divided by the number of rows that
  * have a target if mean != 0 (no row: all gradients zero).  gw is added to if accumulate != 0;
- * either of gx, gw may be NULL.  The gradient of the scores is rounded once to the operands' type (fp32: not rounded)
- * before it meets wt and x.  pass: FFTCONV_FPROP, or FFTCONV_BPROP for the backward call.
+ * either of gx, gw may be NULL.  The gradient of the scores is rounded once to the operands' type (fp32 and
+ * up to eight rows: not rounded) before it meets wt and x.  pass: FFTCONV_FPROP, or FFTCONV_BPROP for the backward call.
  */
 size_t fftconv_xent_workspace_bytes(int pass, int dtype, long N, int D, int V);
 int fftconv_xent_fprop(fftconv_handle hd, int dtype, const void *x, const void *wt, const void *targets, int token_bits,
