@@ -13,15 +13,14 @@
 // 64 whole rows, and the transposing LDS reads turn them on their way to the matrix cores.  So G is
 // written once and nothing is transposed in memory.
 //
-// fp32 operands are terms side by side in the row, and the K loop walks products of terms per 64 k:
+// fp32 operands:
 //
-//  - The scores take two fp16 terms of values scaled row by row to below 2^15 by a power of two, which leaves
-//    the reduction as an exponent (of the row plus of the class): h = fp16(x), l = fp16(x - h), products l h,
-//    h l, h h.  A value is off by 2^-22 of itself or 2^-40 of its row's largest, and what is left out (l l) is
-//    2^-22 of a product: together less than fp32 sums of a few terms lose, at three products.
-//  - The gradients' products reduce over what has no scale of its own (a class's column of G may be tiny in all
-//    rows, and an optimizer will divide by its size): three bf16 terms, whose cut is exact (see split2), at six
-//    products.  What is left out is below 2^-24 of the product of the two.
+//  - The scores are multiplied in fp32 (16x16x4): what a mask puts into a weight (-1e9, the type's lowest value, an
+//    infinity) leaves the other features of its class as they are, which terms of fewer bits do not.  The
+//    tiles are staged as rows of twice as many 16-bit values.  (4096 rows of 1024 features, 32000 classes: 135 TFLOP/s
+//    with all of the call; a library product 153.)
+//  - The gradients' products take three bf16 terms side by side in the row, whose cut is exact (see split2); the K
+//    loop walks six products of terms per 64 k.  What is left out is below 2^-24 of the product of the two.
 //
 // A tile is staged with direct global-to-LDS loads of 16 bytes a lane, one K step ahead, in two
 // buffers.  LDS is written in lane order, so the swizzle that spreads a column of 16-byte pieces over
@@ -51,7 +50,7 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 struct GemmSide {
     const void *p;
     long ld;             // elements from row to row
-    long term;           // elements from one term of an fp32 value to the next
+    long term;           // elements from one of three terms to the next
     long rows;
     int cols;
 };
@@ -65,12 +64,11 @@ struct GemmArgs {
     int places, most;        // rows: blocks the chip holds, steps-bound of the splits; they follow from the live rows
     // stats, grad
     const int *target;       // by row
-    const int *exp_m, *exp_n;    // two terms: exponents of the rows' and classes' scales
     float2 *part;            // [tiles_n][part_ld]: maximum and sum of a row's scores in a tile
     float *hit;              // the target's score, by row
     const float *lse, *coef; // by row
     int n0;                  // class of column 0
-    void *G;                 // (from two terms: in three)
+    void *G;                 // (from fp32 operands: in three terms)
     int twice;               // (small tiles) rows come in pairs: an odd one holds what the rounding of the even one's G left
     long g_ld, g_term;
     long part_ld;
@@ -136,14 +134,22 @@ __device__ __forceinline__ float sixteens_sum(float x) {
     return b.x + b.y;
 }
 
+// parts: matrix instructions for what 16 bytes a lane hold of the reduction.
 template <class T> struct Mfma;
+template <> struct Mfma<float> {
+    typedef floatx4 frag;
+    static constexpr int parts = 4;
+    static __device__ __forceinline__ floatx4 mul(frag a, frag b, floatx4 c, int part) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a[part], b[part], c, 0, 0, 0); }
+};
 template <> struct Mfma<__bf16> {
     typedef bf16x8 frag;
-    static __device__ __forceinline__ floatx4 mul(frag a, frag b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static constexpr int parts = 1;
+    static __device__ __forceinline__ floatx4 mul(frag a, frag b, floatx4 c, int = 0) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct Mfma<_Float16> {
     typedef f16x8 frag;
-    static __device__ __forceinline__ floatx4 mul(frag a, frag b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static constexpr int parts = 1;
+    static __device__ __forceinline__ floatx4 mul(frag a, frag b, floatx4 c, int = 0) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 
 // One operand's tile: R rows of the result's side by 64 k, R * 128 bytes, moved by W waves.
@@ -214,7 +220,7 @@ struct Tile {
     }
 };
 
-constexpr int xent_lds_bytes(int bm, int bn, int wn) { return 2 * (bm + bn) * 128 + 2 * (4 * bm + bn) * 4 + wn * bm * 8; }
+constexpr int xent_lds_bytes(int bm, int bn, int wn) { return 2 * (bm + bn) * 128 + 2 * 3 * bm * 4 + wn * bm * 8; }
 
 // Tiles of FM*WM*16 rows (m) by FN*WN*16 columns (n); a wave has FM*16 by FN*16 of one.  256x256 tiles of eight
 // waves: 128 of a wave's 256 registers are sums, two half steps of fragments 96.  (Four waves of 128x128 spill;
@@ -227,14 +233,14 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
     constexpr int BM = FM * WM * 16, BN = FN * WN * 16, W = WM * WN;
     constexpr bool PIN = END != kClasses, QIN = END == kStats || END == kGrad;
     constexpr bool SCORES = END == kStats || END == kGrad;
-    constexpr int kProducts = TERMS == 3 ? 6 : TERMS == 2 ? 3 : 1;
+    constexpr int kProducts = TERMS == 3 ? 6 : 1;
     typedef typename Mfma<T>::frag F;
     typedef Tile<BM, W, PIN> TP;
     typedef Tile<BN, W, QIN> TQ;
     extern __shared__ __align__(1024) char lds[];
     constexpr int kBytes = (BM + BN) * 128;
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char *)lds;
-    constexpr int kValues = 4 * BM + BN;                                      // of a tile: target, lse, coef, exponents of rows; of columns
+    constexpr int kValues = 3 * BM;                                           // of a tile's rows: target, lse, coef
     char *const values = lds + 2 * kBytes;                                    // [2][kValues]
     float2 *const both = reinterpret_cast<float2 *>(values + 2 * kValues * 4);    // [WN][BM]
 
@@ -276,9 +282,6 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
         if (TERMS == 3) {                                    // l h, h l, m m, m h, h m, h h
             tp_ = t == 0 ? 2 : t == 2 || t == 3 ? 1 : 0;
             tq_ = t == 1 ? 2 : t == 2 || t == 4 ? 1 : 0;
-        } else if (TERMS == 2) {                             // l h, h l, h h
-            tp_ = t == 0;
-            tq_ = t == 1;
         }
         const unsigned to = lds0 + (s & 1) * kBytes;
         tp.load(a.P, a.zeros, k0, tp_, to, w, lane);
@@ -296,10 +299,6 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
                 fetch(a.lse + m0, BM, BM);
                 fetch(a.coef + m0, BM, 2 * BM);
             }
-            if (TERMS == 2) {
-                fetch(a.exp_m + m0, BM, 3 * BM);
-                fetch(a.exp_n + n0, BN, 4 * BM);
-            }
         }
         if (first < last) stage(first);
         if (first + 1 < last) stage(first + 1);
@@ -315,19 +314,21 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
     };
     auto multiply = [&](const Frags &f) {
 #pragma unroll
-        for (int i = 0; i < FM; ++i)
+        for (int part = 0; part < Mfma<T>::parts; ++part)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<T>::mul(f.q[j], f.p[i], acc[i][j]);
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<T>::mul(f.q[j], f.p[i], acc[i][j], part);
     };
     // Reads of one half step between the matrix instructions of the other.
     auto interleave = [&]() {
-        constexpr int reads = FM * (PIN ? 1 : 2) + FN * (QIN ? 1 : 2), each = FM * FN / reads;
+        constexpr int reads = FM * (PIN ? 1 : 2) + FN * (QIN ? 1 : 2), all = FM * FN * Mfma<T>::parts, each = all / reads;
 #pragma unroll
         for (int r = 0; r < reads; ++r) {
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x008, each, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, FM * FN - reads * each, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, all - reads * each, 0);
     };
 
     int u = blockIdx.x, parity = 0;
@@ -379,21 +380,6 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
         const int row = own & 15, quad = (own >> 4) * 4;
         const int *targets = reinterpret_cast<const int *>(values + parity * kValues * 4);
         const float *lses = reinterpret_cast<const float *>(targets) + BM, *coefs = lses + BM;
-        if constexpr (SCORES && TERMS == 2) {
-            const int *exps = targets + 3 * BM;
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int4 n = *reinterpret_cast<const int4 *>(exps + BM + (wn * FN + j) * 16 + quad);
-#pragma unroll
-                for (int i = 0; i < FM; ++i) {
-                    const int m = exps[(wm * FM + i) * 16 + row];
-                    acc[i][j][0] = ldexpf(acc[i][j][0], m + n.x);
-                    acc[i][j][1] = ldexpf(acc[i][j][1], m + n.y);
-                    acc[i][j][2] = ldexpf(acc[i][j][2], m + n.z);
-                    acc[i][j][3] = ldexpf(acc[i][j][3], m + n.w);
-                }
-            }
-        }
         if constexpr (END == kStats) {
             const bool edge = n_at + BN > a.N;
 #pragma unroll
@@ -442,8 +428,8 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
                 if (m_at + r < count) a.part[tn_at * a.part_ld + m_at + r] = v;
             }
         } else if constexpr (END == kGrad) {
-            constexpr int GT = TERMS == 1 ? 1 : 3;            // G's terms
-            T *G = static_cast<T *>(a.G);                    // (two bytes an element in any case)
+            constexpr int GT = sizeof(T) == 4 ? 3 : 1;        // G's terms
+            unsigned short *G = static_cast<unsigned short *>(a.G);
             const bool edge = n_at + BN > a.N || m_at + BM > count;
 #pragma unroll
             for (int i = 0; i < FM; ++i) {

@@ -169,44 +169,27 @@ __global__ __launch_bounds__(kThreads) void xent_place_kernel(ScanArgs a) {
 template <class S>
 struct PackArgs {
     const S *from;
-    S *to;                    // 16-bit types: [rows][ld]
-    _Float16 *two;            // fp32: [rows][2][ld], and the scales' exponents
-    __bf16 *three;            //       [rows][3][ld], where the gradients' products follow
-    int *exps;
+    S *to;                    // [rows][ld], or null
+    __bf16 *three;            // fp32: [rows][3][ld], where the gradients' products follow
     const int *row_of, *count;    // null: rows as they are
     long rows;                // rows behind the count are written as zeros
     int D, ld, T_;            // ld: a multiple of 8, filled with zeros
-    int lanes;                // fp32: threads of a row, a power of two up to 64
 };
 
-template <class T>
-__device__ __forceinline__ void put16(T *to, const T (&t)[8]) { __builtin_memcpy(__builtin_assume_aligned(to, 16), t, 16); }
-
-// The scale 2^-e takes a row whose largest value is `top` to below 2^15; rows that hold nothing but zeros, or
-// something that is not finite, stay.
-__device__ __forceinline__ int scale_exponent(float top) {
-    return top > 0.f && top < INFINITY ? __builtin_amdgcn_frexp_expf(top) - 15 : 0;
-}
-__device__ __forceinline__ void put_terms(const PackArgs<float> &a, long r, int d, const float (&f)[8], int e) {
-    _Float16 h[8], l[8];
+// Eight elements of row r from d on, to where they go.
+template <class S>
+__device__ __forceinline__ void put8(const PackArgs<S> &a, long r, int d, const S (&t)[8]) {
+    if (a.to) __builtin_memcpy(__builtin_assume_aligned(a.to + (size_t)r * a.ld + d, 16), t, sizeof(t));
+    if constexpr (sizeof(S) == 4)
+        if (a.three) {
+            uint4 c[3];
+            split2(t[0], t[1], c[0].x, c[1].x, c[2].x);
+            split2(t[2], t[3], c[0].y, c[1].y, c[2].y);
+            split2(t[4], t[5], c[0].z, c[1].z, c[2].z);
+            split2(t[6], t[7], c[0].w, c[1].w, c[2].w);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float x = ldexpf(f[i], -e);
-        h[i] = (_Float16)x;
-        l[i] = (_Float16)(x - (float)h[i]);
-    }
-    _Float16 *const two = a.two + (size_t)r * 2 * a.ld + d;
-    put16(two, h);
-    put16(two + a.ld, l);
-    if (a.three) {
-        uint4 t[3];
-        split2(f[0], f[1], t[0].x, t[1].x, t[2].x);
-        split2(f[2], f[3], t[0].y, t[1].y, t[2].y);
-        split2(f[4], f[5], t[0].z, t[1].z, t[2].z);
-        split2(f[6], f[7], t[0].w, t[1].w, t[2].w);
-#pragma unroll
-        for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(a.three + (size_t)r * 3 * a.ld + (size_t)q * a.ld + d) = t[q];
-    }
+            for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(a.three + (size_t)r * 3 * a.ld + (size_t)q * a.ld + d) = c[q];
+        }
 }
 
 template <class S>
@@ -219,58 +202,8 @@ __global__ __launch_bounds__(kThreads) void xent_pack_kernel(PackArgs<S> a) {
         const int d = (int)(c - (size_t)r * cpr) * 8;
         S t[8] = {};
         if (r < count) raw8(a.from + (size_t)(a.row_of ? a.row_of[r] : r) * a.D + d, a.D - d, t);
-        put16(a.to + (size_t)r * a.ld + d, t);
+        put8(a, r, d, t);
     }
-}
-
-// fp32: a.lanes threads find a row's largest value, then cut it (it is still in the cache).
-__global__ __launch_bounds__(kThreads) void xent_cut_kernel(PackArgs<float> a) {
-    const long count = a.count ? *a.count : a.rows;
-    const int l = threadIdx.x % a.lanes, rows = kThreads / a.lanes;
-    for (long r0 = (long)blockIdx.x * rows; r0 < a.rows; r0 += (long)gridDim.x * rows) {
-        const long r = r0 + threadIdx.x / a.lanes;
-        if (r >= a.rows) return;
-        const float *const from = r < count ? a.from + (size_t)(a.row_of ? a.row_of[r] : r) * a.D : nullptr;
-        float top = 0.f;
-        if (from)
-            for (int d = l * 8; d < a.D; d += a.lanes * 8) {
-                float f[8];
-                load8(from + d, a.D - d, f);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[i]));
-            }
-        for (int m = 1; m < a.lanes; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-        const int e = scale_exponent(top);
-        if (l == 0) a.exps[r] = e;
-        for (int d = l * 8; d < a.ld; d += a.lanes * 8) {
-            float f[8] = {};
-            if (from) load8(from + d, a.D - d, f);
-            put_terms(a, r, d, f, e);
-        }
-    }
-}
-
-// The largest value of each packed row that lies in planes: 64 rows a block, a quarter of the planes a wave.
-__global__ __launch_bounds__(kThreads) void xent_planes_top_kernel(PackArgs<float> a) {
-    __shared__ float tops[4][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const long r = (long)blockIdx.x * 64 + lane;
-    float top = 0.f;
-    if (r < *a.count) {
-        const RowsOf at{a.D, a.T_};
-        const float *const p = a.from + at.offset(a.row_of[r]);
-        constexpr int U = 16;
-        for (int d = w; d < a.D; d += 4 * U) {
-            float v[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = p[(size_t)(d + 4 * u < a.D ? d + 4 * u : d) * a.T_];
-#pragma unroll
-            for (int u = 0; u < U; ++u) top = fmaxf(top, fabsf(v[u]));
-        }
-    }
-    tops[w][lane] = top;
-    __syncthreads();
-    if (w == 0 && r < a.rows) a.exps[r] = scale_exponent(fmaxf(fmaxf(tops[0][lane], tops[1][lane]), fmaxf(tops[2][lane], tops[3][lane])));
 }
 
 template <class S>
@@ -302,8 +235,7 @@ __global__ __launch_bounds__(kThreads) void xent_pack_planes_kernel(PackArgs<S> 
         S t[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) t[i] = tile[dd + i][q];
-        if constexpr (sizeof(S) == 4) put_terms(a, r0 + q, d0 + dd, t, a.exps[r0 + q]);
-        else put16(a.to + (size_t)(r0 + q) * a.ld + d0 + dd, t);
+        put8(a, r0 + q, d0 + dd, t);
     }
 }
 
@@ -481,11 +413,11 @@ __global__ __launch_bounds__(kThreads) void xent_classes_out_kernel(ClassesOutAr
 // need no packing: one without a target is zeros in LDS.  fp32 is multiplied in fp32 (16x16x4).
 template <class S> struct Thin;
 template <> struct Thin<float> {
-    typedef float frag __attribute__((ext_vector_type(4)));
+    typedef floatx4 frag;
     static constexpr int k = 16;                             // of the reduction per 16 bytes of four lanes
     static __device__ __forceinline__ floatx4 mul(frag a, frag b, floatx4 c) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+        for (int i = 0; i < 4; ++i) c = Mfma<float>::mul(a, b, c, i);
         return c;
     }
 };
@@ -682,7 +614,8 @@ inline long places(const Shape &s) { return s.bm == 256 ? kBigPlaces : kSmallPla
 // Tiles of 256x256 where they fill the chip (one block a CU), of 128x128 (two a CU) where they do not.
 // Where the reduction may be split, it is, until there is a block for every place; such products take
 // tiles 192 columns wide where that covers the columns with less (384 columns: 97 -> 75 us for 15488 rows
-// and 1000 classes in fp32).
+// and 1000 classes in fp32).  fp32 scores take the small tiles: at a sixteenth of the 16-bit rate nothing but the matrix
+// instructions bounds them, and with four to a fragment the large ones spill.
 inline Shape shape_of(long M, long N, long K, int terms, bool split, bool small = false) {
     const long steps = (K + kStep - 1) / kStep, parts = steps * (terms == 3 ? 6 : 1) / 6;      // of six products at least
     Shape s{};
@@ -707,15 +640,15 @@ struct XentPlan {
     int piece, pieces;        // classes a piece
     Shape score, rows, classes;
     int scan_blocks;
-    size_t row_of, pos, target, count, counts, tops, lse, coef, hit, part, x, w, x3, w3, ex, ew, G, gx, gw, total;
+    size_t row_of, pos, target, count, counts, tops, lse, coef, hit, part, x, w, x3, w3, G, gx, gw, total;
 };
 
 // Few rows: as many tiles of 16 of them as a block's LDS holds, four at most.  More groups of rows than one
 // read the weights again; the other path reads them once, but packs the rows, wastes most of a 128-row tile and
-// copies weights whose rows are no whole 16 bytes, or cuts fp32 ones into terms.  32000 classes of 1024 features,
-// us by this path and the other: bf16 18 and 32 (1 row), 28 and 33 (128, two groups), 39 and 37 (192); fp32 35 and
-// 115 (1), 106 and 110 (128, four groups), 153 and 124 (192).  20001 classes of 333 (256 rows, four groups): bf16 36
-// and 38, fp32 52 and 53.
+// copies weights whose rows are no whole 16 bytes.  32000 classes of 1024 features,
+// us by this path and the other: bf16 18 and 32 (1 row), 27 and 33 (128, two groups), 39 and 37 (192); fp32 27 and
+// 86 (1), 57 and 87 (64, two groups), 100 and 87 (128, four groups).  20001 classes of 333 (256 rows, four groups): bf16 35
+// and 36, fp32 51 and 78.
 inline void thin_plan(XentPlan &p, int dtype, long N, int D, int V) {
     const int s = (int)type_bytes(dtype), ks = dtype == kF32 ? 16 : 32;
     const long row = (ceil_to(D, ks) + 16 / s) * s, groups_most = dtype == kF32 || D % 8 ? 4 : 2;
@@ -749,7 +682,7 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
     p.Dp = (int)ceil_to(D, 8);
     p.Dc = (int)ceil_to(D, 4);
     p.terms = dtype == kF32 ? 3 : 1;
-    p.pack_w = dtype == kF32 || D % 8 || !aligned;
+    p.pack_w = D % (16 / (int)type_bytes(dtype)) || !aligned;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at = up(at + bytes, 256); return o; };
     if (!backward) thin_plan(p, dtype, N, D, V);
@@ -765,15 +698,12 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
     p.scan_blocks = (int)((N + kScanRows - 1) / kScanRows);
     p.counts = take((size_t)p.scan_blocks * 4);
     p.tops = take((size_t)p.scan_blocks * 4);
-    const size_t cut = dtype == kF32 ? 2 : 1;            // terms in the scores' product
-    p.x = take((size_t)p.Np * cut * p.Dp * 2);
-    p.w = take(p.pack_w ? (size_t)V * cut * p.Dp * 2 : 0);
-    p.ex = take(cut == 2 ? (size_t)p.Np * 4 : 0);
-    p.ew = take(cut == 2 ? (size_t)ceil_to(V, 256) * 4 : 0);
-    p.x3 = take(backward && cut == 2 ? (size_t)p.Np * 3 * p.Dp * 2 : 0);
-    p.w3 = take(backward && cut == 2 ? (size_t)V * 3 * p.Dp * 2 : 0);
+    p.x = take((size_t)p.Np * p.Dp * type_bytes(dtype));
+    p.w = take(p.pack_w ? (size_t)V * p.Dp * type_bytes(dtype) : 0);
+    p.x3 = take(backward && dtype == kF32 ? (size_t)p.Np * 3 * p.Dp * 2 : 0);
+    p.w3 = take(backward && dtype == kF32 ? (size_t)V * 3 * p.Dp * 2 : 0);
     if (!backward) {
-        p.score = shape_of(N, V, D, p.terms, false);
+        p.score = shape_of(N, V, D, p.terms, false, dtype == kF32);
         p.hit = take((size_t)N * 4);
         p.part = take((size_t)p.score.tiles_n * p.Np * 8);
     } else {
@@ -786,7 +716,7 @@ inline XentPlan xent_plan(bool backward, int dtype, long N, int D, int V, bool a
         p.piece = (int)ceil_to(((long)V + p.pieces - 1) / p.pieces, 256);
         p.pieces = (int)(((long)V + p.piece - 1) / p.piece);
         const long widest = p.piece < V ? p.piece : V;
-        p.score = shape_of(p.R, widest, D, p.terms, false, p.copies == 2);
+        p.score = shape_of(p.R, widest, D, p.terms, false, dtype == kF32 || p.copies == 2);
         p.rows = shape_of(p.R, D, widest, p.terms, true);
         p.classes = shape_of(widest, D, p.R, p.terms, true);
         p.G = take((size_t)p.Np * p.terms * ceil_to(widest, 64) * 2);
@@ -813,7 +743,8 @@ hipError_t product(GemmArgs &g, const Shape &sh, hipStream_t s) {
     };
     if constexpr (END == kRows || END == kClasses)
         if (sh.bn == 192) return launch(xent_gemm_kernel<T, 4, 6, 4, 2, END, TERMS>, 512, xent_lds_bytes(256, 192, 2));
-    if (sh.bm == 256) return launch(xent_gemm_kernel<T, 4, 8, 4, 2, END, TERMS>, 512, xent_lds_bytes(256, 256, 2));
+    if constexpr (sizeof(T) == 2)
+        if (sh.bm == 256) return launch(xent_gemm_kernel<T, 4, 8, 4, 2, END, TERMS>, 512, xent_lds_bytes(256, 256, 2));
     return launch(xent_gemm_kernel<T, 4, 4, 2, 2, END, TERMS>, 256, xent_lds_bytes(128, 128, 2));
 }
 
@@ -831,16 +762,14 @@ inline bool xent_launchable(const XentPlan &p, bool backward, long N, int D, int
     return backward ? product(p.score) && product(p.rows) && product(p.classes) : product(p.score);
 }
 
-// S: the operands' type in memory.  The matrix cores take Score for the scores and Grad for the gradients, in
-// so many terms.
-template <class S> struct Cores { typedef S Score, Grad; static constexpr int score = 1, grad = 1; };
-template <> struct Cores<float> { typedef _Float16 Score; typedef __bf16 Grad; static constexpr int score = 2, grad = 3; };
+// S: the operands' type in memory and in the scores' product.  The gradients' take Grad, in so many terms.
+template <class S> struct Cores { typedef S Grad; static constexpr int terms = 1; };
+template <> struct Cores<float> { typedef __bf16 Grad; static constexpr int terms = 3; };
 
 template <class S>
 struct Xent {
-    typedef typename Cores<S>::Score Score;
     typedef typename Cores<S>::Grad Grad;
-    static constexpr int kScore = Cores<S>::score, kGradTerms = Cores<S>::grad;
+    static constexpr int kGradTerms = Cores<S>::terms, kHalves = sizeof(S) / 2;      // 16-bit values in an element
     const XentCall &c;
     const XentPlan p;
     char *ws;
@@ -864,37 +793,22 @@ struct Xent {
         PackArgs<S> a{};
         a.from = static_cast<const S *>(c.x); a.row_of = at<int>(p.row_of); a.count = at<int>(p.count);
         a.rows = p.Np; a.D = c.D; a.ld = p.Dp; a.T_ = c.T;
+        a.to = at<S>(p.x);
         PackArgs<S> b{};
         b.from = static_cast<const S *>(c.wt); b.rows = c.V; b.D = c.D; b.ld = p.Dp;
-        if constexpr (kScore == 2) {
-            a.two = at<_Float16>(p.x); a.exps = at<int>(p.ex);
-            b.two = at<_Float16>(p.w); b.exps = at<int>(p.ew);
-            if (backward) { a.three = at<__bf16>(p.x3); b.three = at<__bf16>(p.w3); }
-            a.lanes = 1;
-            while (a.lanes < 64 && a.lanes * 8 < p.Dp) a.lanes *= 2;
-            b.lanes = a.lanes;
-            if (c.T) {
-                hipLaunchKernelGGL(xent_planes_top_kernel, dim3((unsigned)(p.Np / 64)), dim3(kThreads), 0, s, a);
-                hipLaunchKernelGGL(xent_pack_planes_kernel<S>, dim3((unsigned)(p.Np / 64 * ((c.D + 63) / 64))), dim3(kThreads), 0, s, a);
-            } else {
-                hipLaunchKernelGGL(xent_cut_kernel, dim3(blocks_for((size_t)p.Np * a.lanes)), dim3(kThreads), 0, s, a);
-            }
-            hipLaunchKernelGGL(xent_cut_kernel, dim3(blocks_for((size_t)c.V * b.lanes)), dim3(kThreads), 0, s, b);
-        } else {
-            a.to = at<S>(p.x);
-            b.to = at<S>(p.w);
-            if (c.T) hipLaunchKernelGGL(xent_pack_planes_kernel<S>, dim3((unsigned)(p.Np / 64 * ((c.D + 63) / 64))), dim3(kThreads), 0, s, a);
-            else hipLaunchKernelGGL(xent_pack_kernel<S>, dim3(blocks_for((size_t)p.Np * p.Dp / 8)), dim3(kThreads), 0, s, a);
-            if (p.pack_w) hipLaunchKernelGGL(xent_pack_kernel<S>, dim3(blocks_for((size_t)c.V * p.Dp / 8)), dim3(kThreads), 0, s, b);
-        }
+        if (p.pack_w) b.to = at<S>(p.w);
+        if (kGradTerms == 3 && backward) { a.three = at<__bf16>(p.x3); b.three = at<__bf16>(p.w3); }
+        if (c.T) hipLaunchKernelGGL(xent_pack_planes_kernel<S>, dim3((unsigned)(p.Np / 64 * ((c.D + 63) / 64))), dim3(kThreads), 0, s, a);
+        else hipLaunchKernelGGL(xent_pack_kernel<S>, dim3(blocks_for((size_t)p.Np * p.Dp / 8)), dim3(kThreads), 0, s, a);
+        if (b.to || b.three) hipLaunchKernelGGL(xent_pack_kernel<S>, dim3(blocks_for((size_t)c.V * p.Dp / 8)), dim3(kThreads), 0, s, b);
         return hipGetLastError();
     }
     // Features and weights (from class v0 on) as the scores' product reads them, and as the gradients' do.
-    GemmSide features() const { return GemmSide{at<Score>(p.x), (long)kScore * p.Dp, p.Dp, p.Np, p.Dp}; }
+    GemmSide features() const { return GemmSide{at<S>(p.x), (long)kHalves * p.Dp, 0, p.Np, kHalves * p.Dp}; }
     GemmSide weights(long v0) const {
-        const long ld = (long)kScore * p.Dp;
-        const Score *w = p.pack_w ? at<Score>(p.w) : static_cast<const Score *>(c.wt);
-        return GemmSide{w + v0 * ld, ld, p.Dp, c.V - v0, p.Dp};
+        const S *const w = p.pack_w ? at<S>(p.w) : static_cast<const S *>(c.wt);
+        const int ld = p.pack_w ? p.Dp : c.D;
+        return GemmSide{w + v0 * ld, (long)kHalves * ld, 0, c.V - v0, kHalves * ld};
     }
     GemmSide grad_features() const { return kGradTerms == 1 ? features() : GemmSide{at<Grad>(p.x3), 3L * p.Dp, p.Dp, p.Np, p.Dp}; }
     GemmSide grad_weights(long v0) const {
@@ -922,11 +836,10 @@ struct Xent {
         if (hipError_t e = pack(false); e != hipSuccess) return e;
         GemmArgs g{};
         g.P = features(); g.Q = weights(0);
-        g.exp_m = at<int>(p.ex); g.exp_n = at<int>(p.ew);
         g.count = sc.count; g.zeros = zeros();
-        g.M = (int)p.Np; g.N = c.V; g.K = c.D;
+        g.M = (int)p.Np; g.N = c.V; g.K = kHalves * c.D;
         g.target = sc.target; g.part = at<float2>(p.part); g.part_ld = p.Np; g.hit = at<float>(p.hit);
-        if (hipError_t e = product<Score, kStats, kScore>(g, p.score, s); e != hipSuccess) return e;
+        if (hipError_t e = product<S, kStats, 1>(g, p.score, s); e != hipSuccess) return e;
         const LossArgs l{g.part, p.Np, p.score.tiles_n, g.hit, sc.row_of, sc.count, c.loss, c.lse};
         hipLaunchKernelGGL(xent_loss_kernel, dim3((unsigned)(p.Np / 64)), dim3(1024), 0, s, l);
         return hipGetLastError();
@@ -948,13 +861,12 @@ struct Xent {
             const GemmSide G{at<Grad>(p.G), p.terms * ld, ld, p.Np, (int)ld};
             GemmArgs g{};
             g.P = features(); g.Q = weights(v0);
-            g.exp_m = at<int>(p.ex); g.exp_n = at<int>(p.ew) + v0;
             g.count = sc.count; g.zeros = zeros();
-            g.M = (int)p.Np; g.N = width; g.K = c.D;
+            g.M = (int)p.Np; g.N = width; g.K = kHalves * c.D;
             g.target = sc.target; g.lse = sc.lse_out; g.coef = sc.coef;
             g.n0 = (int)v0;
             g.G = at<Grad>(p.G); g.g_ld = ld; g.g_term = ld; g.twice = p.copies == 2;
-            if (hipError_t e = product<Score, kGrad, kScore>(g, tiles(p.score, p.R, width), s); e != hipSuccess) return e;
+            if (hipError_t e = product<S, kGrad, 1>(g, tiles(p.score, p.R, width), s); e != hipSuccess) return e;
             if (c.gx) {
                 GemmArgs r{};
                 r.P = G; r.Q = grad_weights(v0);

@@ -1,0 +1,123 @@
+"""The embedding, the linear cross entropy and the gradient norm at values that a mask, a loss scale or an overflow
+brings along.  Bounds as in test_gpu_operators.py, by element: a score that is far from all others counts for nothing, so its
+own error does not either."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_operators import E, TINY, TYPES, gen, half_step, picks, tokens_for, within
+
+pytestmark = pytest.mark.gpu
+LOWEST = torch.finfo(torch.float32).min
+
+
+@pytest.fixture(scope="module")
+def hd(lib):
+    h = lib.Handle(0)
+    yield h
+    h.close()
+
+
+def masked_reference(x, w, tokens):
+    """Loss, lse, gx, gw of the sum of losses in 64 bits and their bounds, for weights of any size and infinite ones."""
+    D, V = x.shape[1], w.shape[0]
+    u, tiny, terms = half_step(x.dtype), TINY[x.dtype], 6 if x.dtype == torch.float32 else 1
+    kept = 0.0 if x.dtype == torch.float32 else u
+    has, at = picks(tokens, V)
+    X, W = x.double(), w.double()
+    z = X @ W.t()
+    lse = torch.logsumexp(z, 1)
+    p = torch.exp(z - lse[:, None])
+    # a score's own error, where its probability is not zero (then z is finite and no further than 800 from lse)
+    dz = torch.where(p > 0, (D + 8) * E * (X.abs() @ W.abs().t()), 0.0)
+    span = torch.where(p > 0, (z - lse[:, None]).abs(), 0.0).amax(1).clamp(max=100.0)
+    dlse = 2 * (p * dz).sum(1) + (3 * span + 4 + V ** 0.5 + 300) * E + 2 * E * lse.abs()
+    rows = torch.arange(len(at), device="cuda")
+    loss = lse - z[rows, at]
+    dloss = torch.where(torch.isfinite(loss), dz[rows, at] + dlse + E * loss.abs(), 0.0)
+    dp = p * ((dz + dlse[:, None]) + (3 * span[:, None] + 6 + lse.abs()[:, None]) * E)
+    p[rows, at] -= 1.0
+    G = p * has[:, None]
+    dG = (dp + (kept + 3 * E) * G.abs()) * has[:, None]
+    low = 2.0 ** -38 if x.dtype == torch.float16 else 0.0
+    dG = dG + torch.where(G == 0, 0.0, low)
+    gx, gw = G @ W, G.t() @ X
+    dgx = dG @ W.abs() + (terms * V + 80) * E * (G.abs() @ W.abs())
+    dgw = dG.t() @ X.abs() + (terms * len(at) + 80) * E * (G.abs().t() @ X.abs())
+    return {"loss": (loss * has, dloss), "lse": (lse * has, dlse), "gx": (gx, dgx + u * (gx.abs() + dgx) + tiny), "gw": (gw, dgw + u * (gw.abs() + dgw) + tiny)}
+
+
+def masked(g, N, D, V, value, gated, dtype=torch.float32):
+    """Feature 0 is a gate, 1 or (every third row, where `gated`) 0; `value` in its weights masks every fifth class."""
+    x, w = torch.randn(N, D, generator=g, device="cuda"), torch.randn(V, D, generator=g, device="cuda")
+    x[:, 0] = 1.0
+    if gated:
+        x[::3, 0] = 0.0
+    w[1::5, 0] = value
+    tokens = tokens_for(g, (N,), V // 5) * 5                 # (classes that are not masked; -500 stands for none as well)
+    return x.to(dtype), w.to(dtype), tokens
+
+
+@pytest.mark.parametrize("N,D,V", [(9, 40, 130), (300, 40, 130), (300, 37, 130), (1500, 200, 1000)])
+@pytest.mark.parametrize("value,gated", [(-math.inf, False), (LOWEST, True), (LOWEST, False), (-1e30, True), (-1e9, True), (-1e5, True)])
+def test_fp32_classes_masked_by_a_weight(hd, N, D, V, value, gated):
+    x, w, tokens = masked(gen(N + D), N, D, V, value, gated)
+    ref = masked_reference(x, w, tokens)
+    loss, lse = hd.xent_fprop(x, w, tokens)
+    within(loss, *ref["loss"], "loss")
+    within(lse, *ref["lse"], "lse")
+    gx, gw = hd.xent_backward(x, w, tokens, lse)
+    within(gw, *ref["gw"], "gw")
+    first = 0 if value >= -1e30 else 1                       # (0 times an infinite weight is not a number)
+    within(gx[:, first:], ref["gx"][0][:, first:], ref["gx"][1][:, first:], "gx")
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:], ids=["bf16", "f16"])
+@pytest.mark.parametrize("N", [6, 300])
+@pytest.mark.parametrize("value", [-math.inf, "lowest"])
+def test_16_bit_classes_masked_by_a_weight(hd, N, value, dtype):
+    value = torch.finfo(dtype).min if value == "lowest" else value
+    x, w, tokens = masked(gen(N), N, 40, 130, value, False, dtype)
+    # (six rows: what the rounding of G leaves is taken along; this bound holds for both)
+    ref = masked_reference(x, w, tokens)
+    loss, lse = hd.xent_fprop(x, w, tokens)
+    within(loss, *ref["loss"], "loss")
+    within(lse, *ref["lse"], "lse")
+    gx, gw = hd.xent_backward(x, w, tokens, lse)
+    within(gw, *ref["gw"], "gw")
+    within(gx[:, 1:], ref["gx"][0][:, 1:], ref["gx"][1][:, 1:], "gx")
+
+
+@pytest.mark.parametrize("N", [9, 300])
+@pytest.mark.parametrize("size", [1e8, 1e15, 1e30])
+def test_fp32_feature_that_meets_zero_weights(hd, N, size):
+    """One feature far above the others, whose weights are zero: the others are what they are without it."""
+    g = gen(60)
+    x, w = torch.randn(N, 48, generator=g, device="cuda"), torch.randn(200, 48, generator=g, device="cuda")
+    x[:, 5], w[:, 5] = size, 0.0
+    tokens = tokens_for(g, (N,), 200)
+    ref = masked_reference(x, w, tokens)
+    loss, lse = hd.xent_fprop(x, w, tokens)
+    within(loss, *ref["loss"], "loss")
+    within(lse, *ref["lse"], "lse")
+    gx, gw = hd.xent_backward(x, w, tokens, lse)
+    within(gx, *ref["gx"], "gx")
+    within(gw, *ref["gw"], "gw")
+
+
+@pytest.mark.parametrize("N", [5, 300])
+@pytest.mark.parametrize("D", [1, 3, 4])
+def test_fp32_scores_of_few_features(hd, N, D):
+    """Scores are fp32 products: with one feature a loss is off by the rounding of a product, not of its factors."""
+    g = gen(61)
+    x, w = torch.randn(N, D, generator=g, device="cuda") * 8, torch.randn(2, D, generator=g, device="cuda") * 8
+    w[1] = 0.0                                               # lse and loss follow one score each
+    tokens = torch.ones(N, dtype=torch.int64, device="cuda")
+    z = x.double() @ w.double().t()
+    want = torch.logsumexp(z, 1)
+    _, lse = hd.xent_fprop(x, w, tokens)
+    # D products and sums of half a step each; the smaller exponential, (3 t + 4) e of exp(-t), and the logarithm, 8 e; the
+    # sum of the larger score and the logarithm, and the result
+    bound = D * E * (x.double().abs() @ w.double().abs().t()).amax(1) + 8 * E + 2 * E * want.abs()
+    within(lse, want, bound, "lse")
