@@ -176,6 +176,20 @@ struct PackArgs {
     int D, ld, T_;            // ld: a multiple of 8, filled with zeros
 };
 
+// (a, b) = h + m + l as split2 cuts them, where a value whose nearest bf16 is infinite goes toward zero: a weight of
+// the type's lowest value is multiplied by gradients of zero.
+__device__ __forceinline__ unsigned finite_high(float v, unsigned h) {
+    const float s = fabsf(v);
+    return s >= 0x1.ffp127f && s < INFINITY ? __builtin_bit_cast(unsigned, v) >> 16 : h;
+}
+__device__ __forceinline__ void cut2(float a, float b, unsigned &h, unsigned &m, unsigned &l) {
+    h = pack_bf16(a, b);
+    h = finite_high(a, h & 0xffff) | finite_high(b, h >> 16) << 16;
+    const float ra = a - low_of(h), rb = b - high_of(h);
+    m = pack_bf16(ra, rb);
+    l = pack_bf16(ra - low_of(m), rb - high_of(m));
+}
+
 // Eight elements of row r from d on, to where they go.
 template <class S>
 __device__ __forceinline__ void put8(const PackArgs<S> &a, long r, int d, const S (&t)[8]) {
@@ -183,10 +197,10 @@ __device__ __forceinline__ void put8(const PackArgs<S> &a, long r, int d, const 
     if constexpr (sizeof(S) == 4)
         if (a.three) {
             uint4 c[3];
-            split2(t[0], t[1], c[0].x, c[1].x, c[2].x);
-            split2(t[2], t[3], c[0].y, c[1].y, c[2].y);
-            split2(t[4], t[5], c[0].z, c[1].z, c[2].z);
-            split2(t[6], t[7], c[0].w, c[1].w, c[2].w);
+            cut2(t[0], t[1], c[0].x, c[1].x, c[2].x);
+            cut2(t[2], t[3], c[0].y, c[1].y, c[2].y);
+            cut2(t[4], t[5], c[0].z, c[1].z, c[2].z);
+            cut2(t[6], t[7], c[0].w, c[1].w, c[2].w);
 #pragma unroll
             for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(a.three + (size_t)r * 3 * a.ld + (size_t)q * a.ld + d) = c[q];
         }

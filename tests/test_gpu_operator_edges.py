@@ -121,3 +121,25 @@ def test_fp32_scores_of_few_features(hd, N, D):
     # sum of the larger score and the logarithm, and the result
     bound = D * E * (x.double().abs() @ w.double().abs().t()).amax(1) + 8 * E + 2 * E * want.abs()
     within(lse, want, bound, "lse")
+
+
+def within_or_beyond(got, ref, bound, what):
+    """Where the bound reaches past fp32's largest value, 2^128, the result may be infinite: a probability of 1 - 1.3e-6
+    times the lowest value is -3.402819e38, and 4.3e32 beside fp32's own lowest, -3.402823e38."""
+    infinite = (got.abs() == math.inf) & (ref.sign() == got.sign()) & (ref.abs() + bound >= -LOWEST)
+    within(torch.where(infinite, ref.float(), got), ref, bound, what)
+
+
+@pytest.mark.parametrize("N,D,V", [(9, 40, 130), (300, 37, 130), (1500, 200, 1000)])
+@pytest.mark.parametrize("value,gated", [(LOWEST, True), (LOWEST, False), (float.fromhex('0x1.ffp127'), False)])
+def test_fp32_gradient_through_weights_near_the_largest_value(hd, N, D, V, value, gated):
+    """A masked class's gradient of zero times its weight is zero.  (The last value is the first whose nearest bf16 is infinite,
+    0x1.ffp127, with a sign that masks where the feature is -1.)"""
+    x, w, tokens = masked(gen(N + D), N, D, V, value, gated)
+    if value > 0:
+        x[:, 0] = -1.0
+    ref = masked_reference(x, w, tokens)
+    _, lse = hd.xent_fprop(x, w, tokens)
+    gx, gw = hd.xent_backward(x, w, tokens, lse)
+    within_or_beyond(gx, *ref["gx"], "gx")
+    within(gw, *ref["gw"], "gw")
