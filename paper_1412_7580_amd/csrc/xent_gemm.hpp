@@ -134,6 +134,10 @@ __device__ __forceinline__ float sixteens_sum(float x) {
     return b.x + b.y;
 }
 
+// What exponentials are taken less of.  Where the largest score is infinite, nothing: sums of nothing but -inf are 0, those with +inf
+// infinite, and so is their logarithm.
+__device__ __forceinline__ float base_of(float top) { return fabsf(top) < INFINITY ? top : 0.f; }
+
 // parts: matrix instructions for what 16 bytes a lane hold of the reduction.
 template <class T> struct Mfma;
 template <> struct Mfma<float> {
@@ -407,7 +411,7 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
 #pragma unroll
                 for (int j = 0; j < FN; ++j) top = fmaxf(fmaxf(fmaxf(top, acc[i][j][0]), acc[i][j][1]), fmaxf(acc[i][j][2], acc[i][j][3]));
                 top = sixteens_max(top);
-                const float base = top == -INFINITY ? 0.f : top;  // (nothing but -inf: the sum is 0)
+                const float base = base_of(top);
                 float sum = 0.f;
 #pragma unroll
                 for (int j = 0; j < FN; ++j)
@@ -422,7 +426,7 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
 #pragma unroll
                 for (int q = 1; q < WN; ++q) {
                     const float2 o = both[q * BM + r];
-                    const float top = fmaxf(v.x, o.x), base = top == -INFINITY ? 0.f : top;
+                    const float top = fmaxf(v.x, o.x), base = base_of(top);
                     v = make_float2(top, v.y * __expf(v.x - base) + o.y * __expf(o.x - base));
                 }
                 if (m_at + r < count) a.part[tn_at * a.part_ld + m_at + r] = v;

@@ -265,7 +265,7 @@ struct LossArgs {
 
 // (maximum, sum of exponentials less that maximum) of two sets of scores taken together.
 __device__ __forceinline__ float2 joined(float2 x, float2 y) {
-    const float top = fmaxf(x.x, y.x), base = top == -INFINITY ? 0.f : top;
+    const float top = fmaxf(x.x, y.x), base = base_of(top);
     return make_float2(top, x.y * __expf(x.x - base) + y.y * __expf(y.x - base));
 }
 
@@ -571,7 +571,7 @@ __global__ __launch_bounds__(kThinThreads, NT < 4 ? 4 : 2) void xent_thin_kernel
                     if (v0 + r >= a.V) acc[t][r] = -INFINITY;
                     high = fmaxf(high, acc[t][r]);
                 }
-                const float m = fmaxf(top[t], high), base = m == -INFINITY ? 0.f : m;
+                const float m = fmaxf(top[t], high), base = base_of(m);
                 float s = sum[t] * __expf(top[t] - base);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s += __expf(acc[t][r] - base);

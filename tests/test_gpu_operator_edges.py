@@ -143,3 +143,30 @@ def test_fp32_gradient_through_weights_near_the_largest_value(hd, N, D, V, value
     gx, gw = hd.xent_backward(x, w, tokens, lse)
     within_or_beyond(gx, *ref["gx"], "gx")
     within(gw, *ref["gw"], "gw")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("N", [6, 300])
+def test_an_infinite_score_makes_the_normaliser_infinite(hd, N, dtype):
+    """log(sum exp z) with one z = +inf is +inf: the loss of any other class is too, that of this class is inf - inf.  A row of
+    nothing but -inf has lse = -inf."""
+    g = gen(70)
+    x, w = torch.randn(N, 24, generator=g, device="cuda"), torch.randn(150, 24, generator=g, device="cuda")
+    x[:, 0] = 0.5
+    x[1, 0], x[2, 0] = 1.0, -1.0
+    x, w = x.to(dtype), w.to(dtype)
+    tokens = torch.arange(N, device="cuda") % 150
+    w[77, 0] = math.inf
+    y = x.clone()
+    y[3:, 0] = 0.0                                           # (0 times infinite: not a number)
+    loss, lse = hd.xent_fprop(x, w, tokens)
+    z = x.double() @ w.double().t()
+    want = torch.logsumexp(z, 1)
+    assert torch.equal(lse == math.inf, want == math.inf) and bool((lse[:2] == math.inf).all()) and bool(torch.isfinite(lse[2]))
+    assert bool((loss[:2] == math.inf).all()) and bool(torch.isfinite(loss[2]))
+    assert all(math.isnan(float(loss[n])) for n in range(77, N, 150))
+    _, lse = hd.xent_fprop(y, w, tokens)
+    assert bool(lse[3:].isnan().all()) and bool((lse[:2] == math.inf).all())
+    w[:, 0] = -math.inf
+    loss, lse = hd.xent_fprop(x, w, tokens)
+    assert bool((lse[:2] == -math.inf).all()) and bool(loss[:2].isnan().all()) and bool((lse[2] == math.inf).all())
