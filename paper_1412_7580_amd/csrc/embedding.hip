@@ -538,6 +538,11 @@ GradPlan grad_plan(int dtype, long N, int D, int V, int T) {
     return p;
 }
 
+// Of the rows' kernel: four chunks a thread, but no fewer than a thousand blocks for it.
+int rows_per_block(long N, int cpr) {
+    const long most = 1024 / cpr, share = (N + 1023) / 1024;
+    return (int)(most < 1 ? 1 : most < share ? most : share);
+}
 long sum_blocks(const GradPlan &p) {
     const long groups = kThreads / p.lanes;
     return (p.chunks * p.slices + groups - 1) / groups;
@@ -550,10 +555,7 @@ hipError_t fprop(const void *table, Tokens tok, void *y, long N, int D, int Tn, 
         hipLaunchKernelGGL(embedding_planes_kernel<T>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
         return hipGetLastError();
     }
-    FpropArgs<T> a{static_cast<const T *>(table), tok, static_cast<T *>(y), N, D, 1, (D + 7) / 8, scale};
-    // four chunks a thread, but no fewer than a thousand blocks for it
-    const long most = 1024 / a.cpr, share = (N + 1023) / 1024;
-    a.rows = (int)(most < 1 ? 1 : most < share ? most : share);
+    FpropArgs<T> a{static_cast<const T *>(table), tok, static_cast<T *>(y), N, D, rows_per_block(N, (D + 7) / 8), (D + 7) / 8, scale};
     hipLaunchKernelGGL(embedding_rows_kernel<T>, dim3((unsigned)((N + a.rows - 1) / a.rows)), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
@@ -623,12 +625,18 @@ hipError_t accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, 
 
 size_t embedding_accgrad_bytes(int dtype, long N, int D, int V, int T) { return N ? grad_plan(dtype, N, D, V, T).total : 0; }
 
-bool embedding_fits(bool accgrad, long N, int D, int V, int T) {
+bool embedding_fits(bool accgrad, int dtype, long N, int D, int V, int T) {
     if (N == 0) return true;
-    if (T && (double)N / T * ((T + 63) / 64) * ((D + 63) / 64) > 0x7fffffff) return false;
-    if (!accgrad) return true;
-    const GradPlan p = grad_plan(kF32, N, D, V, T);
-    return p.chunks <= 0x7fffffff && sum_blocks(p) <= 0x7fffffff && (double)V * D * 4 / kZeroBytes + p.sort.blocks + 1 <= 0x7fffffff;
+    if (T && !grid_fits((double)(N / T) * ((T + 63) / 64) * ((D + 63) / 64), kThreads)) return false;
+    if (!accgrad) {
+        const int rows = rows_per_block(N, (D + 7) / 8);
+        return T || grid_fits((double)((N + rows - 1) / rows), kThreads);
+    }
+    const GradPlan p = grad_plan(dtype, N, D, V, T);
+    // (a sorting launch clears its share of the table: this many blocks and up to one for what does not divide)
+    const double clearing = (double)V * D * type_bytes(dtype) / kZeroBytes / (p.sort.one ? 1 : 2 * p.sort.passes) + 1;
+    return grid_fits((p.sort.one ? 1 : p.sort.blocks) + clearing, kSortThreads) && grid_fits((double)sum_blocks(p), kThreads) &&
+           grid_fits((double)p.chunks, kThreads);
 }
 
 hipError_t launch_embedding_fprop(int dtype, const void *table, Tokens tok, void *y, long N, int D, int T, float scale, hipStream_t s) {

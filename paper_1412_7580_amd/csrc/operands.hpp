@@ -11,6 +11,9 @@ enum { kF32 = 0, kBF16 = 1, kF16 = 2 };
 inline size_t type_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
 inline size_t up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 inline long ceil_to(long v, long a) { return (v + a - 1) / a * a; }
+// Whether one launch takes so many blocks: it has fewer than 2^32 threads.  (In floating point: sizes up to 2^30 multiply
+// beyond 64 bits.)
+inline bool grid_fits(double blocks, int threads) { return blocks * threads < 0x1p32; }
 
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(__bf16 v) { return (float)v; }
@@ -75,7 +78,7 @@ struct RowsOf {
 
 // ---- embedding.hip
 size_t embedding_accgrad_bytes(int dtype, long N, int D, int V, int T);
-bool embedding_fits(bool accgrad, long N, int D, int V, int T);              // whether one launch takes each of its grids
+bool embedding_fits(bool accgrad, int dtype, long N, int D, int V, int T);   // whether one launch takes each of its grids
 hipError_t launch_embedding_fprop(int dtype, const void *table, Tokens tok, void *y, long N, int D, int T, float scale, hipStream_t s);
 hipError_t launch_embedding_accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, int D, int T, float scale,
                                     bool accumulate, void *ws, hipStream_t s);

@@ -114,14 +114,14 @@ int fftconv_embedding_fprop(fftconv_handle hd, int dtype, const void *table, con
     if (int rc = check_sizes(dtype, token_bits, N, D, V, T); rc != FFTCONV_OK) return rc;
     if (N == 0) return FFTCONV_OK;
     if (!table || !tokens || !y) return FFTCONV_INVALID_ARG;
-    if (!embedding_fits(false, N, D, V, T)) return FFTCONV_UNSUPPORTED;
+    if (!embedding_fits(false, dtype, N, D, V, T)) return FFTCONV_UNSUPPORTED;
     const OnDevice on(hd->device);
     if (on.error != hipSuccess) return hip_fail(hd, on.error);
     return done(hd, launch_embedding_fprop(dtype, table, Tokens{tokens, token_bits == 64, V}, y, N, D, T, scale, hd->stream));
 }
 
 size_t fftconv_embedding_workspace_bytes(int dtype, long N, int D, int V, int T) {
-    if (check_sizes(dtype, 64, N, D, V, T) != FFTCONV_OK) return 0;
+    if (check_sizes(dtype, 64, N, D, V, T) != FFTCONV_OK || !embedding_fits(true, dtype, N, D, V, T)) return 0;
     return embedding_accgrad_bytes(dtype, N, D, V, T);
 }
 
@@ -130,7 +130,7 @@ int fftconv_embedding_accgrad(fftconv_handle hd, int dtype, const void *gy, cons
     if (!hd || !gtable) return FFTCONV_INVALID_ARG;
     if (int rc = check_sizes(dtype, token_bits, N, D, V, T); rc != FFTCONV_OK) return rc;
     if (N > 0 && (!gy || !tokens)) return FFTCONV_INVALID_ARG;
-    if (!embedding_fits(true, N, D, V, T)) return FFTCONV_UNSUPPORTED;
+    if (!embedding_fits(true, dtype, N, D, V, T)) return FFTCONV_UNSUPPORTED;
     const OnDevice on(hd->device);
     if (on.error != hipSuccess) return hip_fail(hd, on.error);
     if (N > 0)
@@ -141,6 +141,7 @@ int fftconv_embedding_accgrad(fftconv_handle hd, int dtype, const void *gy, cons
 
 size_t fftconv_xent_workspace_bytes(int pass, int dtype, long N, int D, int V) {
     if (check_sizes(dtype, 64, N, D, V, 0) != FFTCONV_OK || D > kMostFeatures || (pass != FFTCONV_FPROP && pass != FFTCONV_BPROP)) return 0;
+    if (!xent_fits(pass == FFTCONV_BPROP, dtype, N, D, V, 0)) return 0;
     return xent_bytes(pass == FFTCONV_BPROP, dtype, N, D, V, false);
 }
 

@@ -270,7 +270,8 @@ __device__ __forceinline__ float2 joined(float2 x, float2 y) {
 }
 
 // 64 rows a block; sixteen threads a row join its tiles' maxima and sums.
-__global__ __launch_bounds__(1024) void xent_loss_kernel(LossArgs a) {
+constexpr int kLossThreads = 1024;
+__global__ __launch_bounds__(kLossThreads) void xent_loss_kernel(LossArgs a) {
     __shared__ float2 both[16][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, count = *a.count;
     const long m = (long)blockIdx.x * 64 + lane;
@@ -769,11 +770,12 @@ inline unsigned blocks_for(size_t chunks) {
 
 // Whether every launch of a call takes its grid.
 inline bool xent_launchable(const XentPlan &p, bool backward, long N, int D, int T) {
-    const auto fits = [](double blocks) { return blocks <= 0x7fffffff; };
     if (p.thin_tiles) return true;                           // (a thousand rows at most)
-    if (T && (!fits((double)(p.Np / 64) * ((D + 63) / 64)) || !fits((double)N / T * ((T + 63) / 64) * ((D + 63) / 64)))) return false;
-    const auto product = [&](const Shape &s) { return fits((double)s.tiles_m * s.tiles_n * s.most); };
-    return backward ? product(p.score) && product(p.rows) && product(p.classes) : product(p.score);
+    if (T && !grid_fits((double)(p.Np / 64) * ((D + 63) / 64), kThreads)) return false;
+    const auto product = [&](const Shape &s) { return (double)s.tiles_m * s.tiles_n * s.most <= 0x7fffffff; };      // (counted by its blocks)
+    if (!backward) return product(p.score) && grid_fits((double)(p.Np / 64), kLossThreads);
+    if (T && !grid_fits((double)(N / T) * ((T + 63) / 64) * ((D + 63) / 64), kThreads)) return false;
+    return product(p.score) && product(p.rows) && product(p.classes);
 }
 
 // S: the operands' type in memory and in the scores' product.  The gradients' take Grad, in so many terms.
@@ -855,7 +857,7 @@ struct Xent {
         g.target = sc.target; g.part = at<float2>(p.part); g.part_ld = p.Np; g.hit = at<float>(p.hit);
         if (hipError_t e = product<S, kStats, 1>(g, p.score, s); e != hipSuccess) return e;
         const LossArgs l{g.part, p.Np, p.score.tiles_n, g.hit, sc.row_of, sc.count, c.loss, c.lse};
-        hipLaunchKernelGGL(xent_loss_kernel, dim3((unsigned)(p.Np / 64)), dim3(1024), 0, s, l);
+        hipLaunchKernelGGL(xent_loss_kernel, dim3((unsigned)(p.Np / 64)), dim3(kLossThreads), 0, s, l);
         return hipGetLastError();
     }
 
