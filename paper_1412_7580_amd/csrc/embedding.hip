@@ -552,12 +552,10 @@ hipError_t fprop(const void *table, Tokens tok, void *y, long N, int D, int Tn, 
     if (Tn) {
         PlaneArgs<T> a{static_cast<const T *>(table), tok, static_cast<T *>(y), D, Tn, (Tn + 63) / 64, (D + 63) / 64, scale};
         const long blocks = N / Tn * a.tiles_t * a.tiles_d;
-        hipLaunchKernelGGL(embedding_planes_kernel<T>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
-        return hipGetLastError();
+        return run(embedding_planes_kernel<T>, dim3((unsigned)blocks), kThreads, 0, s, a);
     }
     FpropArgs<T> a{static_cast<const T *>(table), tok, static_cast<T *>(y), N, D, rows_per_block(N, (D + 7) / 8), (D + 7) / 8, scale};
-    hipLaunchKernelGGL(embedding_rows_kernel<T>, dim3((unsigned)((N + a.rows - 1) / a.rows)), dim3(kThreads), 0, s, a);
-    return hipGetLastError();
+    return run(embedding_rows_kernel<T>, dim3((unsigned)((N + a.rows - 1) / a.rows)), kThreads, 0, s, a);
 }
 
 template <class T>
@@ -569,7 +567,7 @@ hipError_t accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, 
     if (Tn) {
         TurnArgs<T> t{rows, tok, reinterpret_cast<T *>(ws + p.rows), D, Tn, (Tn + 63) / 64, (D + 63) / 64};
         const long blocks = N / Tn * t.tiles_t * t.tiles_d;
-        hipLaunchKernelGGL(planes_to_rows_kernel<T>, dim3((unsigned)blocks), dim3(kThreads), 0, s, t);
+        if (hipError_t e = run(planes_to_rows_kernel<T>, dim3((unsigned)blocks), kThreads, 0, s, t); e != hipSuccess) return e;
         rows = t.rows;
     }
     SortArgs so{};
@@ -591,8 +589,8 @@ hipError_t accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, 
     if (p.sort.one) {
         so.first = 1;
         const unsigned grid = 1 + clear(0);
-        if (N <= 1024) hipLaunchKernelGGL(sort_block_kernel<1>, dim3(grid), dim3(kSortThreads), 0, s, so);
-        else hipLaunchKernelGGL(sort_block_kernel<4>, dim3(grid), dim3(kSortThreads), 0, s, so);
+        const auto kernel = N <= 1024 ? sort_block_kernel<1> : sort_block_kernel<4>;
+        if (hipError_t e = run(kernel, dim3(grid), kSortThreads, 0, s, so); e != hipSuccess) return e;
     } else {
         for (int i = 0; i < p.sort.passes; ++i) {
             so.first = i == 0;
@@ -602,10 +600,11 @@ hipError_t accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, 
             so.key_out = reinterpret_cast<int *>(ws + p.key[i & 1]);
             so.idx_out = reinterpret_cast<int *>(ws + p.idx[i & 1]);
             unsigned grid = so.blocks + clear(2 * i);
-            hipLaunchKernelGGL(sort_count_kernel, dim3(grid), dim3(kSortThreads), 0, s, so);
-            if (so.placed) hipLaunchKernelGGL(sort_columns_kernel, dim3(((1 << so.bits) + 63) / 64), dim3(kSortThreads), 0, s, so);
+            if (hipError_t e = run(sort_count_kernel, dim3(grid), kSortThreads, 0, s, so); e != hipSuccess) return e;
+            if (so.placed)
+                if (hipError_t e = run(sort_columns_kernel, dim3(((1 << so.bits) + 63) / 64), kSortThreads, 0, s, so); e != hipSuccess) return e;
             grid = so.blocks + clear(2 * i + 1);
-            hipLaunchKernelGGL(sort_place_kernel, dim3(grid), dim3(kSortThreads), 0, s, so);
+            if (hipError_t e = run(sort_place_kernel, dim3(grid), kSortThreads, 0, s, so); e != hipSuccess) return e;
         }
     }
     SumArgs<T> a{};
@@ -616,9 +615,8 @@ hipError_t accgrad(int dtype, const void *gy, Tokens tok, void *gtable, long N, 
     a.tail = reinterpret_cast<float *>(ws + p.tail);
     a.chunks = p.chunks; a.D = D; a.C = p.C; a.lanes = p.lanes; a.slices = p.slices;
     a.scale = scale; a.accumulate = accumulate;
-    hipLaunchKernelGGL(embedding_sum_kernel<T>, dim3((unsigned)sum_blocks(p)), dim3(kThreads), 0, s, a);
-    if (p.chunks > 1) hipLaunchKernelGGL(embedding_join_kernel<T>, dim3((unsigned)p.chunks), dim3(kThreads), 0, s, a);
-    return hipGetLastError();
+    if (hipError_t e = run(embedding_sum_kernel<T>, dim3((unsigned)sum_blocks(p)), kThreads, 0, s, a); e != hipSuccess) return e;
+    return p.chunks > 1 ? run(embedding_join_kernel<T>, dim3((unsigned)p.chunks), kThreads, 0, s, a) : hipSuccess;
 }
 
 }  // namespace
@@ -652,9 +650,8 @@ hipError_t launch_embedding_accgrad(int dtype, const void *gy, Tokens tok, void 
         if (accumulate) return hipSuccess;
         const size_t n = (size_t)tok.V * D;
         const unsigned blocks = (unsigned)(n / kThreads + 1 < 4096 ? n / kThreads + 1 : 4096);
-        if (dtype == kF32) hipLaunchKernelGGL(zero_kernel<float>, dim3(blocks), dim3(kThreads), 0, s, static_cast<float *>(gtable), n);
-        else hipLaunchKernelGGL(zero_kernel<__bf16>, dim3(blocks), dim3(kThreads), 0, s, static_cast<__bf16 *>(gtable), n);
-        return hipGetLastError();
+        if (dtype == kF32) return run(zero_kernel<float>, dim3(blocks), kThreads, 0, s, static_cast<float *>(gtable), n);
+        return run(zero_kernel<__bf16>, dim3(blocks), kThreads, 0, s, static_cast<__bf16 *>(gtable), n);
     }
     char *w = static_cast<char *>(ws);
     if (dtype == kF32) return accgrad<float>(dtype, gy, tok, gtable, N, D, T, scale, accumulate, w, s);

@@ -163,7 +163,7 @@ long pieces_of(int count, const long *sizes, long piece) {
 }
 
 template <int CAP>
-void launch(int count, const void *const *grads, const long *sizes, const int *dtypes, void *const *out, float max_norm,
+hipError_t launch(int count, const void *const *grads, const long *sizes, const int *dtypes, void *const *out, float max_norm,
             float *norm, void *ws, long piece, long pieces, hipStream_t s) {
     NormArgs<CAP> a;
     a.piece = piece;
@@ -189,11 +189,11 @@ void launch(int count, const void *const *grads, const long *sizes, const int *d
             }
             a.first[a.count] = n;
             if (!a.count) break;
-            if (clip) hipLaunchKernelGGL(clip_kernel<CAP>, dim3(n), dim3(kThreads), 0, s, a);
-            else hipLaunchKernelGGL(norm_kernel<CAP>, dim3(n), dim3(kThreads), 0, s, a);
+            if (hipError_t e = run(clip ? clip_kernel<CAP> : norm_kernel<CAP>, dim3(n), kThreads, 0, s, a); e != hipSuccess) return e;
             base += n;
         }
     }
+    return hipSuccess;
 }
 
 }  // namespace
@@ -205,11 +205,10 @@ size_t grad_norm_bytes(int count, const long *sizes) {
 hipError_t launch_grad_norm(int count, const void *const *grads, const long *sizes, const int *dtypes, void *const *out,
                             float max_norm, float *norm, void *ws, hipStream_t s) {
     const long piece = piece_length(count, sizes), pieces = pieces_of(count, sizes, piece);
-    if (count <= kFew) launch<kFew>(count, grads, sizes, dtypes, out, max_norm, norm, ws, piece, pieces, s);
-    else launch<kPerLaunch>(count, grads, sizes, dtypes, out, max_norm, norm, ws, piece, pieces, s);
-    if (!out || !pieces)
-        hipLaunchKernelGGL(norm_end_kernel, dim3(1), dim3(kThreads), 0, s, static_cast<const double *>(ws), (int)pieces, norm);
-    return hipGetLastError();
+    const auto lists = count <= kFew ? launch<kFew> : launch<kPerLaunch>;
+    if (hipError_t e = lists(count, grads, sizes, dtypes, out, max_norm, norm, ws, piece, pieces, s); e != hipSuccess) return e;
+    if (out && pieces) return hipSuccess;
+    return run(norm_end_kernel, dim3(1), kThreads, 0, s, static_cast<const double *>(ws), (int)pieces, norm);
 }
 
 }  // namespace fc

@@ -15,6 +15,15 @@ inline long ceil_to(long v, long a) { return (v + a - 1) / a * a; }
 // beyond 64 bits.)
 inline bool grid_fits(double blocks, int threads) { return blocks * threads < 0x1p32; }
 
+// One launch and its own error, whatever an earlier HIP call of the caller's left.  What follows reads what it writes: a
+// chain of launches ends with the first that fails.
+template <class P> struct Same { typedef P type; };
+template <class... P>
+hipError_t run(void (*kernel)(P...), dim3 grid, int threads, size_t lds, hipStream_t s, const typename Same<P>::type &...p) {
+    void *args[] = {const_cast<void *>(static_cast<const void *>(&p))...};
+    return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(threads), args, lds, s);
+}
+
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(__bf16 v) { return (float)v; }
 __device__ __forceinline__ float to_float(_Float16 v) { return (float)v; }

@@ -753,8 +753,7 @@ hipError_t product(GemmArgs &g, const Shape &sh, hipStream_t s) {
     const dim3 grid((unsigned)(tiles < g.places ? tiles : g.places));
     const auto launch = [&](auto kernel, int threads, int lds) {
         if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(kernel), lds); e != hipSuccess) return e;
-        hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, s, g);
-        return hipGetLastError();
+        return run(kernel, grid, threads, lds, s, g);
     };
     if constexpr (END == kRows || END == kClasses)
         if (sh.bn == 192) return launch(xent_gemm_kernel<T, 4, 6, 4, 2, END, TERMS>, 512, xent_lds_bytes(256, 192, 2));
@@ -798,12 +797,13 @@ struct Xent {
     template <class P> P *at(size_t o) const { return reinterpret_cast<P *>(ws + o); }
     const void *zeros() const { return ws + p.count + 16; }
 
-    void scan(ScanArgs &sc) {
+    hipError_t scan(ScanArgs &sc) {
         sc.tok = c.tok; sc.N = c.N; sc.blocks = p.scan_blocks; sc.copies = p.copies;
         sc.counts = at<int>(p.counts); sc.tops = at<float>(p.tops);
         sc.row_of = at<int>(p.row_of); sc.target = at<int>(p.target); sc.count = at<int>(p.count); sc.zeros = at<uint4>(p.count + 16);
-        if (sc.blocks > kScanInline) hipLaunchKernelGGL(xent_count_kernel, dim3(sc.blocks), dim3(kThreads), 0, s, sc);
-        hipLaunchKernelGGL(xent_place_kernel, dim3(sc.blocks), dim3(kThreads), 0, s, sc);
+        if (sc.blocks > kScanInline)
+            if (hipError_t e = run(xent_count_kernel, dim3(sc.blocks), kThreads, 0, s, sc); e != hipSuccess) return e;
+        return run(xent_place_kernel, dim3(sc.blocks), kThreads, 0, s, sc);
     }
     hipError_t pack(bool backward) {
         PackArgs<S> a{};
@@ -814,10 +814,10 @@ struct Xent {
         b.from = static_cast<const S *>(c.wt); b.rows = c.V; b.D = c.D; b.ld = p.Dp;
         if (p.pack_w) b.to = at<S>(p.w);
         if (kGradTerms == 3 && backward) { a.three = at<__bf16>(p.x3); b.three = at<__bf16>(p.w3); }
-        if (c.T) hipLaunchKernelGGL(xent_pack_planes_kernel<S>, dim3((unsigned)(p.Np / 64 * ((c.D + 63) / 64))), dim3(kThreads), 0, s, a);
-        else hipLaunchKernelGGL(xent_pack_kernel<S>, dim3(blocks_for((size_t)p.Np * p.Dp / 8)), dim3(kThreads), 0, s, a);
-        if (b.to || b.three) hipLaunchKernelGGL(xent_pack_kernel<S>, dim3(blocks_for((size_t)c.V * p.Dp / 8)), dim3(kThreads), 0, s, b);
-        return hipGetLastError();
+        const hipError_t e = c.T ? run(xent_pack_planes_kernel<S>, dim3((unsigned)(p.Np / 64 * ((c.D + 63) / 64))), kThreads, 0, s, a)
+                                 : run(xent_pack_kernel<S>, dim3(blocks_for((size_t)p.Np * p.Dp / 8)), kThreads, 0, s, a);
+        if (e != hipSuccess || (!b.to && !b.three)) return e;
+        return run(xent_pack_kernel<S>, dim3(blocks_for((size_t)c.V * p.Dp / 8)), kThreads, 0, s, b);
     }
     // Features and weights (from class v0 on) as the scores' product reads them, and as the gradients' do.
     GemmSide features() const { return GemmSide{at<S>(p.x), (long)kHalves * p.Dp, 0, p.Np, kHalves * p.Dp}; }
@@ -835,9 +835,9 @@ struct Xent {
     hipError_t thin_tiles(const ThinArgs<S> &a) {
         auto k = xent_thin_kernel<S, NT>;
         if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(k), p.thin_lds); e != hipSuccess) return e;
-        hipLaunchKernelGGL(k, dim3(p.thin_blocks, (unsigned)((c.N + NT * 16 - 1) / (NT * 16))), dim3(kThinThreads), p.thin_lds, s, a);
-        hipLaunchKernelGGL(xent_thin_loss_kernel<S>, dim3((unsigned)c.N), dim3(kThreads), 0, s, a);
-        return hipGetLastError();
+        const dim3 grid(p.thin_blocks, (unsigned)((c.N + NT * 16 - 1) / (NT * 16)));
+        if (hipError_t e = run(k, grid, kThinThreads, p.thin_lds, s, a); e != hipSuccess) return e;
+        return run(xent_thin_loss_kernel<S>, dim3((unsigned)c.N), kThreads, 0, s, a);
     }
     hipError_t thin() {
         const ThinArgs<S> a{static_cast<const S *>(c.x), static_cast<const S *>(c.wt), c.tok, c.N, c.D, c.V, c.T, p.thin_blocks,
@@ -848,7 +848,7 @@ struct Xent {
         if (p.thin_tiles) return thin();
         ScanArgs sc{};
         sc.loss = c.loss; sc.lse = c.lse;
-        scan(sc);
+        if (hipError_t e = scan(sc); e != hipSuccess) return e;
         if (hipError_t e = pack(false); e != hipSuccess) return e;
         GemmArgs g{};
         g.P = features(); g.Q = weights(0);
@@ -857,8 +857,7 @@ struct Xent {
         g.target = sc.target; g.part = at<float2>(p.part); g.part_ld = p.Np; g.hit = at<float>(p.hit);
         if (hipError_t e = product<S, kStats, 1>(g, p.score, s); e != hipSuccess) return e;
         const LossArgs l{g.part, p.Np, p.score.tiles_n, g.hit, sc.row_of, sc.count, c.loss, c.lse};
-        hipLaunchKernelGGL(xent_loss_kernel, dim3((unsigned)(p.Np / 64)), dim3(kLossThreads), 0, s, l);
-        return hipGetLastError();
+        return run(xent_loss_kernel, dim3((unsigned)(p.Np / 64)), kLossThreads, 0, s, l);
     }
 
     hipError_t backward() {
@@ -868,7 +867,7 @@ struct Xent {
         sc.lse_out = at<float>(p.lse); sc.coef = at<float>(p.coef);
         sc.alpha = at<float>(p.count + 4);
         sc.scale = c.scale; sc.mean = c.mean; sc.half_range = c.dtype == kF16;
-        scan(sc);
+        if (hipError_t e = scan(sc); e != hipSuccess) return e;
         if (hipError_t e = pack(true); e != hipSuccess) return e;
         for (int i = 0; i < p.pieces; ++i) {
             const long v0 = (long)i * p.piece;
@@ -905,23 +904,21 @@ struct Xent {
                 if (hipError_t e = product<Grad, kClasses, kGradTerms>(w, sh, s); e != hipSuccess) return e;
                 if (sh.splits > 1) {
                     const ClassesOutArgs<S> o{at<float>(p.gw), sc.alpha, gw, width, p.Dc, sh.splits, c.D, c.accumulate};
-                    hipLaunchKernelGGL(xent_classes_out_kernel<S>, dim3(blocks_for((size_t)width * ((c.D + 7) / 8))), dim3(kThreads), 0, s, o);
+                    const dim3 grid(blocks_for((size_t)width * ((c.D + 7) / 8)));
+                    if (hipError_t e = run(xent_classes_out_kernel<S>, grid, kThreads, 0, s, o); e != hipSuccess) return e;
                 }
             }
         }
-        if (c.gx) {
-            const RowsOutArgs<S> o{at<float>(p.gx), sc.pos, sc.count, sc.alpha, static_cast<S *>(c.gx), c.N, p.Dc,
-                                   p.rows.bm, p.rows.tiles_n, (int)places(p.rows), p.rows.most, c.D, c.T, p.copies};
-            if (c.T) {
-                const long blocks = c.N / c.T * ((c.T + 63) / 64) * ((c.D + 63) / 64);
-                hipLaunchKernelGGL(xent_planes_out_kernel<S>, dim3((unsigned)blocks), dim3(kThreads), 0, s, o);
-            } else {
-                const size_t pieces = (size_t)c.N * ((c.D + 7) / 8);
-                if (p.rows.splits > 8) hipLaunchKernelGGL((xent_rows_out_kernel<S, 8>), dim3(blocks_for(pieces * 8)), dim3(kThreads), 0, s, o);
-                else hipLaunchKernelGGL((xent_rows_out_kernel<S, 1>), dim3(blocks_for(pieces)), dim3(kThreads), 0, s, o);
-            }
+        if (!c.gx) return hipSuccess;
+        const RowsOutArgs<S> o{at<float>(p.gx), sc.pos, sc.count, sc.alpha, static_cast<S *>(c.gx), c.N, p.Dc,
+                               p.rows.bm, p.rows.tiles_n, (int)places(p.rows), p.rows.most, c.D, c.T, p.copies};
+        if (c.T) {
+            const long blocks = c.N / c.T * ((c.T + 63) / 64) * ((c.D + 63) / 64);
+            return run(xent_planes_out_kernel<S>, dim3((unsigned)blocks), kThreads, 0, s, o);
         }
-        return hipGetLastError();
+        const size_t pieces = (size_t)c.N * ((c.D + 7) / 8);
+        if (p.rows.splits > 8) return run(xent_rows_out_kernel<S, 8>, dim3(blocks_for(pieces * 8)), kThreads, 0, s, o);
+        return run(xent_rows_out_kernel<S, 1>, dim3(blocks_for(pieces)), kThreads, 0, s, o);
     }
     // The last piece may be narrower than the plan's.
     static Shape tiles(Shape sh, long M, long N) {

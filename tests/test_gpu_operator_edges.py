@@ -170,3 +170,21 @@ def test_an_infinite_score_makes_the_normaliser_infinite(hd, N, dtype):
     w[:, 0] = -math.inf
     loss, lse = hd.xent_fprop(x, w, tokens)
     assert bool((lse[:2] == -math.inf).all()) and bool(loss[:2].isnan().all()) and bool((lse[2] == math.inf).all())
+
+
+def test_an_error_that_an_earlier_call_left_is_not_this_call_s(hd):
+    """A refused hipSetDevice leaves its error for the next hipGetLastError of the thread; launches that go well say so."""
+    import ctypes
+    g = gen(71)
+    x, w, t = torch.randn(300, 24, generator=g, device="cuda"), torch.randn(50, 24, generator=g, device="cuda"), tokens_for(g, (300,), 50)
+    y, gt, gw, loss, norm = torch.empty_like(x), torch.empty_like(w), torch.empty_like(w), torch.empty(300, device="cuda"), torch.empty((), device="cuda")
+    lse = hd.xent_fprop(x, w, t)[1]
+    with open("/proc/self/maps") as f:
+        runtime = ctypes.CDLL(next(line.split()[-1] for line in f if "libamdhip64" in line))
+    for call in (lambda: hd.embedding_fprop(w, t, y=y), lambda: hd.embedding_accgrad(x, t, 50, gtable=gt), lambda: hd.xent_fprop(x, w, t, loss=loss, lse=lse),
+                 lambda: hd.xent_backward(x, w, t, lse, want_gx=False, gw=gw), lambda: hd.grad_norm([x, w], norm=norm), lambda: hd.grad_clip([x, w], 1.0, norm=norm)):
+        call()                                               # (what this allocates is there)
+        assert runtime.hipSetDevice(4096) != 0
+        call()
+    runtime.hipGetLastError()
+    torch.cuda.synchronize()
