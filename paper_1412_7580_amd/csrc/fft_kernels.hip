@@ -4,17 +4,20 @@
 #include "fft_kernels_impl.hpp"
 
 #include <cstdlib>
+#include <map>
 #include <mutex>
-#include <unordered_map>
+#include <utility>
 
 namespace fc {
 
 hipError_t allow_big_lds(const void *fn, size_t bytes) {
     if (bytes <= 64 * 1024) return hipSuccess;
     static std::mutex mu;
-    static std::unordered_map<const void *, size_t> granted;
+    static std::map<std::pair<int, const void *>, size_t> granted;      // the attribute is the current device's
+    int device = 0;
+    if (const hipError_t e = hipGetDevice(&device); e != hipSuccess) return e;
     std::lock_guard<std::mutex> lock(mu);
-    size_t &have = granted[fn];
+    size_t &have = granted[{device, fn}];
     if (have >= bytes) return hipSuccess;
     const size_t ask = 160 * 1024;   // the whole LDS of a gfx950 compute unit
     const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)ask);
