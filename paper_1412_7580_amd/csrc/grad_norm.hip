@@ -105,10 +105,13 @@ __global__ __launch_bounds__(kThreads) void norm_end_kernel(const double *sums, 
     if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
-// The factor is c * c2: one below fp32's normal range (2^-126) would lose bits that the results have.
-struct Factor { float c, c2; };
-template <class T>
-__device__ __forceinline__ void scaled(const T *in, T *out, long n, Factor k) {
+// WIDE: a factor below fp32's normal range (2^-126) would lose bits that the results have; it is multiplied in 64 bits.
+template <bool WIDE>
+__device__ __forceinline__ float product(float v, double factor) {
+    return WIDE ? (float)((double)v * factor) : v * (float)factor;
+}
+template <bool WIDE, class T>
+__device__ __forceinline__ void scaled(const T *in, T *out, long n, double factor) {
     constexpr int U = 4;
     long i = (long)threadIdx.x * 8;
     for (; i + (U - 1) * kThreads * 8L + 8 <= n; i += U * kThreads * 8L) {
@@ -118,7 +121,7 @@ __device__ __forceinline__ void scaled(const T *in, T *out, long n, Factor k) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[u][j] = f[u][j] * k.c * k.c2;
+            for (int j = 0; j < 8; ++j) f[u][j] = product<WIDE>(f[u][j], factor);
             store8(out + i + u * kThreads * 8L, 8, f[u]);
         }
     }
@@ -127,9 +130,16 @@ __device__ __forceinline__ void scaled(const T *in, T *out, long n, Factor k) {
         float f[8];
         load8(in + i, m, f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = f[j] * k.c * k.c2;
+        for (int j = 0; j < 8; ++j) f[j] = product<WIDE>(f[j], factor);
         store8(out + i, m, f);
     }
+}
+template <class T>
+__device__ __forceinline__ void scaled(const void *in, void *out, long from, long n, double factor) {
+    const T *const i = static_cast<const T *>(in) + from;
+    T *const o = static_cast<T *>(out) + from;
+    if (factor < 0x1p-126) scaled<true>(i, o, n, factor);
+    else scaled<false>(i, o, n, factor);
 }
 
 // The pieces are walked from the last one back: the end of what the norm read is still in the cache.
@@ -139,15 +149,14 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(NormArgs<CAP> a) {
     const double norm = sqrt(total(a.sums, a.pieces, lds));
     if (a.base == 0 && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
     const bool clip = norm > (double)a.max_norm && (float)norm < INFINITY;
-    const double whole = clip ? (double)a.max_norm / norm : 1.0;
-    const Factor c = whole < 0x1p-126 ? Factor{(float)(whole * 0x1p100), 0x1p-100f} : Factor{(float)whole, 1.f};
+    const double factor = clip ? (double)a.max_norm / norm : 1.0;
     const int p = (int)(gridDim.x - 1 - blockIdx.x), t = tensor_of(a, p);
     if (!clip && a.in[t] == a.out[t]) return;
     const long from = (long)(p - a.first[t]) * a.piece;
     const long n = a.size[t] - from < a.piece ? a.size[t] - from : a.piece;
-    if (a.dtype[t] == kF32) scaled(static_cast<const float *>(a.in[t]) + from, static_cast<float *>(a.out[t]) + from, n, c);
-    else if (a.dtype[t] == kBF16) scaled(static_cast<const __bf16 *>(a.in[t]) + from, static_cast<__bf16 *>(a.out[t]) + from, n, c);
-    else scaled(static_cast<const _Float16 *>(a.in[t]) + from, static_cast<_Float16 *>(a.out[t]) + from, n, c);
+    if (a.dtype[t] == kF32) scaled<float>(a.in[t], a.out[t], from, n, factor);
+    else if (a.dtype[t] == kBF16) scaled<__bf16>(a.in[t], a.out[t], from, n, factor);
+    else scaled<_Float16>(a.in[t], a.out[t], from, n, factor);
 }
 
 long piece_length(int count, const long *sizes) {

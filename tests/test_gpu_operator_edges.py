@@ -188,3 +188,14 @@ def test_an_error_that_an_earlier_call_left_is_not_this_call_s(hd):
         call()
     runtime.hipGetLastError()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("n", [4, 8192])
+@pytest.mark.parametrize("value,max_norm", [(5e37, 1e-37), (1.6e38, 3e-38), (5e37, 1e-44), (1e38, 2.0 ** -126)])
+def test_clipping_by_factors_down_to_the_smallest(hd, value, max_norm, n):
+    """Four equal elements, of norm twice theirs: each becomes max_norm / 2, off by the rounding of a product, or half the smallest step."""
+    t = torch.zeros(n, device="cuda")
+    t[:4] = value
+    limit = float(torch.tensor(max_norm))
+    hd.grad_clip([t], max_norm)
+    assert float((t[:4].double() - limit / 2).abs().max()) <= 2 * E * limit / 2 + 2.0 ** -150 and float(t[4:].abs().sum()) == 0
