@@ -832,7 +832,7 @@ class Handle:
 
     def _norm_result(self, grads, norm):
         if norm is None:
-            norm = grads[0].new_empty((), dtype=torch.float32) if grads else torch.empty((), device=f"cuda:{self.device}")
+            norm = grads[0].new_empty((), dtype=torch.float32) if grads else torch.empty((), dtype=torch.float32, device=f"cuda:{self.device}")
             return norm, norm.data_ptr()
         return norm, self._typed(norm, torch.float32, (), "norm")
 

@@ -199,3 +199,15 @@ def test_clipping_by_factors_down_to_the_smallest(hd, value, max_norm, n):
     limit = float(torch.tensor(max_norm))
     hd.grad_clip([t], max_norm)
     assert float((t[:4].double() - limit / 2).abs().max()) <= 2 * E * limit / 2 + 2.0 ** -150 and float(t[4:].abs().sum()) == 0
+
+
+@pytest.mark.parametrize("default", [torch.float64, torch.bfloat16])
+def test_the_norm_of_an_empty_list_is_float32_under_any_default_type(hd, default):
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(default)
+    try:
+        norms = hd.grad_norm([]), hd.grad_clip([], 1.0)
+    finally:
+        torch.set_default_dtype(before)
+    for n in norms:
+        assert n.dtype == torch.float32 and float(n) == 0
