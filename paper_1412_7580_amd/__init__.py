@@ -148,6 +148,19 @@ def _check(rc: int, what: str):
         raise FFTConvError(f"{what}: {msg} (status {rc})")
 
 
+_MOST = 1 << 30       # rows, features and classes of the operators
+
+
+def _sizes_fit(*sizes):
+    """Whether the C entry points may take these sizes: ctypes would wrap those beyond an int into others."""
+    return all(0 <= n <= _MOST for n in sizes)
+
+
+def _check_sizes(what, *sizes):
+    if not _sizes_fit(*sizes):
+        raise FFTConvError(f"{what}: sizes must be from 0 to 2^30, not {sizes}")
+
+
 def _dev_f32(t, name):
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.float32 and t.is_contiguous()):
         raise FFTConvError(f"{name} must be a contiguous float32 tensor in device memory")
@@ -719,6 +732,8 @@ class Handle:
         return (s[0], D) + s[1:], T
 
     def embedding_workspace_bytes(self, dtype, N, D, V, T=0) -> int:
+        if not _sizes_fit(N, D, V, T):
+            return 0
         return int(self._lib.fftconv_embedding_workspace_bytes(_types[dtype], N, D, V, T))
 
     def embedding_fprop(self, table, tokens, scale=1.0, planes=False, y=None):
@@ -730,6 +745,7 @@ class Handle:
         V, D = table.shape
         t, bits = self._tokens(tokens, "tokens")
         shape, T = self._feature_shape(tokens, D, planes, "tokens")
+        _check_sizes("fftconv_embedding_fprop", tokens.numel(), D, V, T)
         if y is None:
             y = table.new_empty(shape)
             to = y.data_ptr()
@@ -750,6 +766,7 @@ class Handle:
         shape, T = self._feature_shape(tokens, D, planes, "tokens")
         if gy.shape != shape:
             raise FFTConvError("gy and tokens disagree")
+        _check_sizes("fftconv_embedding_accgrad", tokens.numel(), D, V, T)
         if gtable is None:
             if accumulate:
                 raise FFTConvError("accumulate needs an existing gtable")
@@ -763,6 +780,8 @@ class Handle:
         return gtable
 
     def xent_workspace_bytes(self, pass_, dtype, N, D, V) -> int:
+        if not _sizes_fit(N, D, V):
+            return 0
         return int(self._lib.fftconv_xent_workspace_bytes(pass_, _types[dtype], N, D, V))
 
     def _classifier(self, x, wt, targets, planes):
@@ -775,6 +794,7 @@ class Handle:
         shape, T = self._feature_shape(targets, D, planes, "targets")
         if x.shape != shape:
             raise FFTConvError("x, wt and targets disagree")
+        _check_sizes("the cross entropy", targets.numel(), D, V, T)
         return (k, px, pw, pt, bits), (targets.numel(), D, V, T)
 
     def xent_fprop(self, x, wt, targets, planes=False, loss=None, lse=None, ws=None):
