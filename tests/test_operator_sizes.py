@@ -46,7 +46,7 @@ def test_sizes_that_the_library_does_not_take(hd, size):
                  lambda: hd.embedding_accgrad(fake(3, 1), t, size), lambda: hd.embedding_accgrad(fake(1, size), one, 5),
                  lambda: hd.xent_fprop(fake(3, 2), fake(size, 2), t), lambda: hd.xent_fprop(fake(1, size), fake(2, size), one),
                  lambda: hd.xent_backward(fake(3, 2), fake(size, 2), t, fake(3))):
-        with pytest.raises(pkg.FFTConvError, match="2\^30"):
+        with pytest.raises(pkg.FFTConvError, match="2\\^30"):
             call()
     # and their workspaces are of no bytes, as the library's own size functions say
     assert hd.embedding_workspace_bytes(torch.float32, 3, 1, size) == 0 and hd.embedding_workspace_bytes(torch.float32, 3, size, 5) == 0
