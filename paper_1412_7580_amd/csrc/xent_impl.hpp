@@ -132,9 +132,7 @@ __global__ __launch_bounds__(kThreads) void xent_place_kernel(ScanArgs a) {
     if (a.half_range) {
         if (!a.gloss) top = 1.f;
         if (top > 0.f && top < INFINITY) e2 = 14 - (ilogbf(top) + 1);
-        e2 = e2 < -100 ? -100 : e2 > 100 ? 100 : e2;
     }
-    const float up = ldexpf(1.f, e2);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const long n = n0 + tid * 4 + e;
@@ -147,7 +145,7 @@ __global__ __launch_bounds__(kThreads) void xent_place_kernel(ScanArgs a) {
                 a.target[q] = r.t[e];
                 if (a.coef) {
                     a.lse_out[q] = a.lse_in[n];
-                    a.coef[q] = (a.gloss ? a.gloss[n] : 1.f) * up;
+                    a.coef[q] = ldexpf(a.gloss ? a.gloss[n] : 1.f, e2);
                 }
             }
             ++at;
@@ -159,7 +157,8 @@ __global__ __launch_bounds__(kThreads) void xent_place_kernel(ScanArgs a) {
     if (blockIdx.x == 0 && tid == 0) {
         *a.count = total * a.copies;
         *a.zeros = make_uint4(0, 0, 0, 0);
-        if (a.alpha) *a.alpha = total ? ldexpf(a.mean ? a.scale / (float)total : a.scale, -e2) : 0.f;
+        // (in 64 bits: a scale of 2^-140 is still whole when 2^140 comes to it)
+        if (a.alpha) *a.alpha = total ? (float)ldexp(a.mean ? (double)a.scale / total : (double)a.scale, -e2) : 0.f;
     }
 }
 

@@ -211,3 +211,18 @@ def test_the_norm_of_an_empty_list_is_float32_under_any_default_type(hd, default
         torch.set_default_dtype(before)
     for n in norms:
         assert n.dtype == torch.float32 and float(n) == 0
+
+
+@pytest.mark.parametrize("N", [7, 90])
+@pytest.mark.parametrize("k", [-131, -123, -110, -101, 88, 101, 110, 118, 127])
+def test_xent_half_gradients_of_every_loss_scale(hd, N, k):
+    """dL/dloss of 2^k and a scale that takes it back: the gradients are those of k = 0."""
+    g = gen(72)
+    x = torch.randn(N, 48, generator=g, device="cuda").half()
+    w = torch.randn(200, 48, generator=g, device="cuda").mul_(0.3).half()
+    tokens = tokens_for(g, (N,), 200, none=0.1)
+    _, lse = hd.xent_fprop(x, w, tokens)
+    for mean in (False, True):
+        base = hd.xent_backward(x, w, tokens, lse, gloss=torch.full((N,), 1.0, device="cuda"), scale=0.0625, mean=mean)
+        got = hd.xent_backward(x, w, tokens, lse, gloss=torch.full((N,), 2.0 ** k, device="cuda"), scale=0.0625 * 2.0 ** -k, mean=mean)
+        assert torch.equal(got[0], base[0]) and torch.equal(got[1], base[1])
