@@ -43,9 +43,11 @@ __global__ __launch_bounds__(kThreads) void embedding_rows_kernel(FpropArgs<T> a
         const int d = (int)(c - r * a.cpr) * 8, n = a.D - d;
         const int t = a.tok(n0 + r);
         float f[8] = {};
-        if (t >= 0) load8(a.table + (size_t)t * a.D + d, n, f);
+        if (t >= 0) {                                        // (else zero, whatever the scale)
+            load8(a.table + (size_t)t * a.D + d, n, f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] *= a.scale;
+            for (int i = 0; i < 8; ++i) f[i] *= a.scale;
+        }
         store8(a.y + (size_t)(n0 + r) * a.D + d, n, f);
     }
 }
@@ -72,7 +74,11 @@ __global__ __launch_bounds__(kThreads) void embedding_planes_kernel(PlaneArgs<T>
         float f[8] = {};
         if (t0 + r < a.T_ && d < a.D) {
             const int v = a.tok((long)s * a.T_ + t0 + r);
-            if (v >= 0) load8(a.table + (size_t)v * a.D + d, a.D - d, f);
+            if (v >= 0) {
+                load8(a.table + (size_t)v * a.D + d, a.D - d, f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] *= a.scale;
+            }
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) tile[(c & 7) * 8 + i][r] = f[i];
@@ -81,7 +87,7 @@ __global__ __launch_bounds__(kThreads) void embedding_planes_kernel(PlaneArgs<T>
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     if (t0 + lane < a.T_)
         for (int i = w; i < 64 && d0 + i < a.D; i += kWaves)
-            a.y[((size_t)s * a.D + d0 + i) * a.T_ + t0 + lane] = (T)(tile[i][lane] * a.scale);
+            a.y[((size_t)s * a.D + d0 + i) * a.T_ + t0 + lane] = (T)tile[i][lane];
 }
 
 // The turn back: planes of gy to rows, for accGrad (rows without a token are not needed and skipped).

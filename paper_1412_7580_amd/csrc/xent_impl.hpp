@@ -361,8 +361,9 @@ __global__ __launch_bounds__(kThreads) void xent_rows_out_kernel(RowsOutArgs<S> 
 #pragma unroll
                 for (int i = 0; i < 8; ++i) f[i] += sums[q * B + threadIdx.x][i];
         }
+        if (at >= 0)                                         // (else zero, whatever the scale)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] *= alpha;
+            for (int i = 0; i < 8; ++i) f[i] *= alpha;
         if (c < total) store8(a.gx + (size_t)n * a.D + d, a.D - d, f);
     }
 }
@@ -380,10 +381,14 @@ __global__ __launch_bounds__(kThreads) void xent_planes_out_kernel(RowsOutArgs<S
         float f[8] = {};
         if (t0 + q < a.T_ && d0 + dd < a.D) {
             const int at = a.pos[(long)s * a.T_ + t0 + q];
-            if (at >= 0) sum_row(a, parts, at, d0 + dd, 0, parts.splits, f);
+            if (at >= 0) {
+                sum_row(a, parts, at, d0 + dd, 0, parts.splits, f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] *= alpha;
+            }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) tile[dd + i][q] = f[i] * alpha;
+        for (int i = 0; i < 8; ++i) tile[dd + i][q] = f[i];
     }
     __syncthreads();
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;

@@ -226,3 +226,28 @@ def test_xent_half_gradients_of_every_loss_scale(hd, N, k):
         base = hd.xent_backward(x, w, tokens, lse, gloss=torch.full((N,), 1.0, device="cuda"), scale=0.0625, mean=mean)
         got = hd.xent_backward(x, w, tokens, lse, gloss=torch.full((N,), 2.0 ** k, device="cuda"), scale=0.0625 * 2.0 ** -k, mean=mean)
         assert torch.equal(got[0], base[0]) and torch.equal(got[1], base[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("scale", [math.inf, math.nan])
+@pytest.mark.parametrize("shape,planes", [((3, 70), False), ((3, 70), True), ((6,), False)])
+def test_rows_without_a_token_are_zero_under_any_scale(hd, shape, planes, scale, dtype):
+    """A loss scale that has overflowed: what takes no part stays zero, all else is infinite or not a number."""
+    g = gen(73)
+    V, D = 40, 24
+    tokens = tokens_for(g, shape, V, none=0.3)
+    tokens.view(-1)[:2] = torch.tensor([-1, 5], device="cuda")
+    has, _ = picks(tokens, V)
+    table = torch.randn(V, D, generator=g, device="cuda").to(dtype)
+    y = hd.embedding_fprop(table, tokens, scale=scale, planes=planes)
+    rows = y.flatten(2).transpose(1, 2).reshape(-1, D) if planes else y.reshape(-1, D)
+    assert bool((rows[~has] == 0).all()) and not bool(torch.isfinite(rows[has]).any())
+    x = torch.randn(y.shape, generator=g, device="cuda").to(dtype)
+    gt = hd.embedding_accgrad(x, tokens, V, scale=scale, planes=planes)
+    named = torch.zeros(V, dtype=torch.bool, device="cuda")
+    named[tokens[(tokens >= 0)]] = True
+    assert bool((gt[~named] == 0).all()) and not bool(torch.isfinite(gt[named]).any())
+    _, lse = hd.xent_fprop(x, table, tokens, planes=planes)
+    gx, _ = hd.xent_backward(x, table, tokens, lse, scale=scale, planes=planes)
+    rows = gx.flatten(2).transpose(1, 2).reshape(-1, D) if planes else gx.reshape(-1, D)
+    assert bool((rows[~has] == 0).all()) and not bool(torch.isfinite(rows[has]).any())
