@@ -422,8 +422,8 @@ int fftconv_xent_backward(fftconv_handle hd, int dtype, const void *x, const voi
  * The 2-norm of `count` tensors taken together (host arrays of device pointers, element counts and types;
  * read during the call only), into norm[0] on the device.  grad_clip also writes
  * out[i] = grads[i] * min(1, max_norm / norm); out[i] has the type of grads[i], and may be grads[i] itself.  A
- * norm that is infinite (in fp32) or not a number leaves the values as they are.  Outputs that overlap each other, or
- * another tensor's input, and a max_norm that is not positive and finite give FFTCONV_INVALID_ARG.
+ * norm that is infinite (in fp32) or not a number leaves the values as they are.  Outputs (norm among them) that overlap each
+ * other, or another tensor's input, and a max_norm that is not positive and finite give FFTCONV_INVALID_ARG.
  */
 size_t fftconv_grad_workspace_bytes(int count, const long *sizes);
 int fftconv_grad_norm(fftconv_handle hd, int count, const void *const *grads, const long *sizes, const int *dtypes, float *norm,

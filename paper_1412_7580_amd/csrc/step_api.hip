@@ -73,11 +73,12 @@ int check_list(int count, const void *const *grads, const long *sizes, const int
 }
 
 // No element may be written twice, nor be read as another tensor's after it was written.
-int check_apart(int count, const void *const *grads, const long *sizes, const int *dtypes, void *const *out) {
+int check_apart(int count, const void *const *grads, const long *sizes, const int *dtypes, void *const *out, const float *norm) {
     struct Range { size_t from, to; int tensor; bool written; };
     Range *r = new (std::nothrow) Range[2 * (size_t)count + 1];
     if (!r) return FFTCONV_HIP_ERROR;
     int n = 0;
+    r[n++] = Range{(size_t)norm, (size_t)norm + sizeof(float), count, true};
     for (int i = 0; i < count; ++i) {
         if (!sizes[i]) continue;
         const size_t bytes = (size_t)sizes[i] * type_bytes(dtypes[i]), in = (size_t)grads[i], to = (size_t)out[i];
@@ -204,7 +205,7 @@ int fftconv_grad_clip(fftconv_handle hd, int count, const void *const *grads, co
     if (int rc = check_list(count, grads, sizes, dtypes); rc != FFTCONV_OK) return rc;
     for (int i = 0; i < count; ++i)
         if (sizes[i] > 0 && !out[i]) return FFTCONV_INVALID_ARG;
-    if (int rc = check_apart(count, grads, sizes, dtypes, out); rc != FFTCONV_OK) return rc;
+    if (int rc = check_apart(count, grads, sizes, dtypes, out, norm); rc != FFTCONV_OK) return rc;
     return run_norm(hd, count, grads, sizes, dtypes, out, max_norm, norm, ws, ws_bytes);
 }
 
