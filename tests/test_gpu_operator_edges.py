@@ -251,3 +251,50 @@ def test_rows_without_a_token_are_zero_under_any_scale(hd, shape, planes, scale,
     gx, _ = hd.xent_backward(x, table, tokens, lse, scale=scale, planes=planes)
     rows = gx.flatten(2).transpose(1, 2).reshape(-1, D) if planes else gx.reshape(-1, D)
     assert bool((rows[~has] == 0).all()) and not bool(torch.isfinite(rows[has]).any())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("N,D,V", [(5, 4470, 300), (5, 5001, 300), (260, 8200, 130), (3, 1 << 20, 5), (130, 1 << 20, 5)])
+def test_xent_of_long_rows(hd, N, D, V, dtype):
+    g = gen(74)
+    x = torch.randn(N, D, generator=g, device="cuda").to(dtype)
+    w = (torch.randn(V, D, generator=g, device="cuda") * (2 / math.sqrt(D))).to(dtype)
+    tokens = tokens_for(g, (N,), V, none=0.1)
+    tokens[0] = 3
+    ref = masked_reference(x, w, tokens)
+    loss, lse = hd.xent_fprop(x, w, tokens)
+    within(loss, *ref["loss"], "loss")
+    within(lse, *ref["lse"], "lse")
+    gx, gw = hd.xent_backward(x, w, tokens, lse)
+    within(gx, *ref["gx"], "gx")
+    within(gw, *ref["gw"], "gw")
+
+
+def test_xent_of_rows_too_long_is_refused(hd, lib):
+    x, w, t = torch.zeros(1, (1 << 20) + 1, device="cuda"), torch.zeros(2, (1 << 20) + 1, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    with pytest.raises(lib.FFTConvError, match="unsupported"):
+        hd.xent_fprop(x, w, t)
+    with pytest.raises(lib.FFTConvError, match="unsupported"):
+        hd.xent_backward(x, w, t, torch.zeros(1, device="cuda"))
+
+
+@pytest.mark.parametrize("N", [3000, 40000])
+def test_embedding_of_a_table_whose_tokens_take_four_digits(hd, N):
+    """2^25 rows and tokens at both ends: whole numbers, exact in any order."""
+    V = (1 << 25) + 3
+    tokens = torch.randint(0, V, (N,), generator=gen(75), device="cuda")
+    tokens[::7], tokens[1::7], tokens[2::7] = V - 1, 0, 1 << 24
+    gy = torch.arange(N, device="cuda").float()[:, None] % 64
+    got = hd.embedding_accgrad(gy, tokens, V)
+    want = torch.zeros(V, 1, device="cuda").index_add_(0, tokens, gy)
+    assert torch.equal(got, want)
+
+
+def test_norm_and_clip_beyond_32_bit_offsets(hd):
+    n = (1 << 31) + 12345
+    t = torch.zeros(n, device="cuda", dtype=torch.bfloat16)
+    t[0], t[1 << 30], t[-1] = 3.0, 4.0, 12.0
+    assert float(hd.grad_norm([t])) == 13.0
+    assert float(hd.grad_clip([t], 6.5)) == 13.0
+    assert [float(t[i]) for i in (0, 1 << 30, n - 1)] == [1.5, 2.0, 6.0]
+    assert float(hd.grad_norm([t])) == 6.5
