@@ -153,11 +153,11 @@ _MOST = 1 << 30       # rows, features and classes of the operators
 
 def _sizes_fit(*sizes):
     """Whether the C entry points may take these sizes: ctypes would wrap those beyond an int into others."""
-    return all(0 <= n <= _MOST for n in sizes)
+    return max(sizes) <= _MOST and min(sizes) >= 0
 
 
 def _check_sizes(what, *sizes):
-    if not _sizes_fit(*sizes):
+    if max(sizes) > _MOST or min(sizes) < 0:
         raise FFTConvError(f"{what}: sizes must be from 0 to 2^30, not {sizes}")
 
 
