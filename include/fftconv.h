@@ -409,7 +409,10 @@ int fftconv_embedding_accgrad(fftconv_handle hd, int dtype, const void *gy, cons
  * of the loss  scale * sum_n gloss[n] loss[n]  (gloss NULL: all ones), divided by the number of rows that
  * have a target if mean != 0 (no row: all gradients zero).  gw is added to if accumulate != 0;
  * either of gx, gw may be NULL.  The gradient of the scores is rounded once to the operands' type (fp32 and
- * up to eight rows: not rounded) before it meets wt and x.  pass: FFTCONV_FPROP, or FFTCONV_BPROP for the backward call.
+ * up to eight rows: not rounded) before it meets wt and x.  Scores are sums of fp32 products whatever the type; fp32 gradients
+ * are formed from three bf16 terms of each value: what is left out is below 2^-24 of a product, and of a value below 2^-110 what
+ * is below 2^-134.  pass: FFTCONV_FPROP, or FFTCONV_BPROP for the backward call, whose workspace in fp32 holds up to 10 bytes for
+ * each element of x and wt.
  */
 size_t fftconv_xent_workspace_bytes(int pass, int dtype, long N, int D, int V);
 int fftconv_xent_fprop(fftconv_handle hd, int dtype, const void *x, const void *wt, const void *targets, int token_bits,

@@ -10,8 +10,9 @@
 // depend on the order in which blocks run.  The list of tensors travels in the kernel's arguments, so
 // nothing is copied to the device and a captured call holds its list itself.
 //
-// 400 million bf16 elements: norm 178 us (4.5 TB/s), scaling 309 (1.6 GB, 5.2 TB/s: the last of what the norm read
-// comes from the cache); a copy runs at 4.8.
+// 400 million bf16 elements: norm 175 us (4.6 TB/s), scaling 307 (1.6 GB, 5.2 TB/s: the last of what the norm read
+// comes from the cache); a copy runs at 4.8.  (Adding up all pieces in every block costs their number squared: 6 of 24 ms
+// for 50000 tensors, nothing for hundreds.)
 //
 // A norm that is zero, infinite in fp32 or not a number leaves the tensors as they are: the caller sees it in `norm`.
 #include "operands.hpp"

@@ -12,8 +12,6 @@
 // the scores formed twice, which costs a third more operations and saves 4 N V bytes written and read.
 // With 8192 rows, 2048 features and 65536 classes in bf16 the step takes 6.9 ms: 1270 TFLOP/s over all four,
 // where a library product of that size and layout reaches 1300 (1270 and 1090 for the gradients' layouts).
-// Steps without the staging or the LDS reads show what bounds it: the matrix instructions alone take 71 % of
-// the time, LDS reads 11 %, staging 18 %.
 //
 // Rows without a target are taken out before anything else: the rows that have one are packed, so a
 // padded batch costs what its filled part costs, and nothing of the other rows is read (whatever
