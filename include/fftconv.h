@@ -382,8 +382,9 @@ const char *fftconv_last_kernel_label(fftconv_handle h, int i);
  *  - T = 0: features are rows [N, D].  T > 0: they are planes [N / T, D, T], the BDHW tensors of
  *    the passes with T = h * w positions and D planes; tokens and losses are [N / T, T] then.
  *  - Rows, features, classes: up to 2^30 each (features of xent: 2^20), and no more at once than the grid of one
- *    launch takes (2^32 threads: of 64-position tiles of planes, 2^24), else FFTCONV_UNSUPPORTED, and 0 from the size functions.  N = 0 is a no-op, except
- *    that a gradient which is not accumulated becomes zero.
+ *    launch takes (2^32 threads: of 64-position tiles of planes, 2^24), else FFTCONV_UNSUPPORTED; the size functions give
+ *    0 then (that of xent, which is not told T, as for rows).  N = 0 is a no-op, except that a gradient which is not
+ *    accumulated becomes zero.
  *  - Results do not depend on the order in which workgroups run: the same call gives the same bits.
  *  - The calls run on the handle's device, whichever is current.  `ws`: 16-byte aligned device scratch
  *    of at least the size function's bytes, or NULL for a buffer of the handle's (not the one of the passes, which a

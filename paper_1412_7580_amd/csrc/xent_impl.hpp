@@ -664,8 +664,8 @@ struct XentPlan {
 // read the weights again; the other path reads them once, but packs the rows, wastes most of a 128-row tile and
 // copies weights whose rows are no whole 16 bytes.  32000 classes of 1024 features,
 // us by this path and the other: bf16 18 and 32 (1 row), 27 and 33 (128, two groups), 39 and 37 (192); fp32 27 and
-// 86 (1), 57 and 87 (64, two groups), 100 and 87 (128, four groups).  20001 classes of 333 (256 rows, four groups): bf16 35
-// and 36, fp32 51 and 78.
+// 86 (1), 57 and 85 (64, two groups), 100 and 85 (128, four groups; 34 and 80 with 5000 classes).  20001 classes of 333 (256 rows,
+// four groups): bf16 35 and 36, fp32 51 and 78.
 inline void thin_plan(XentPlan &p, int dtype, long N, int D, int V) {
     const int s = (int)type_bytes(dtype), ks = dtype == kF32 ? 16 : 32;
     const long row = (ceil_to(D, ks) + 16 / s) * s, groups_most = dtype == kF32 || D % 8 ? 4 : 2;
