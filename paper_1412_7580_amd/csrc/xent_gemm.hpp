@@ -38,7 +38,6 @@ namespace fc {
 
 enum { kStats = 0, kGrad = 1, kRows = 2, kClasses = 3 };
 constexpr int kStep = 64;            // k per step
-constexpr float kLog2E = 1.44269504088896340736f;
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
@@ -440,7 +439,7 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
                 const int lm = (wm * FM + i) * 16 + row;
                 const long m = m_at + lm;
                 const int rel = targets[lm] - a.n0 - (int)n_at - wn * FN * 16 - quad;
-                const float lse = lses[lm], coef = coefs[lm], lse2 = lse * kLog2E;
+                const float lse = lses[lm], coef = coefs[lm];
                 const bool hit = m < count && rel >= 0 && rel < FN * 16 && (rel & 12) == 0;
                 const bool any = __any(hit);
                 // Two column tiles at a time: lanes of odd sixteens trade theirs of the first tile for the second's of
@@ -452,10 +451,9 @@ __global__ __launch_bounds__(WM *WN * 64) void xent_gemm_kernel(GemmArgs a) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         float g[4];
-                        // (for 16-bit operands one instruction less: off by the rounding of lse log2(e), as lse is by its own)
+                        // (the difference first: it is exact where the two are close, and so is a probability of one)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            g[r] = GT == 3 ? __expf(acc[i][j + h][r] - lse) : __builtin_amdgcn_exp2f(fmaf(acc[i][j + h][r], kLog2E, -lse2));
+                        for (int r = 0; r < 4; ++r) g[r] = __expf(acc[i][j + h][r] - lse);
                         if (any)
 #pragma unroll
                             for (int r = 0; r < 4; ++r) g[r] -= hit && rel == (j + h) * 16 + r ? 1.f : 0.f;

@@ -298,3 +298,29 @@ def test_norm_and_clip_beyond_32_bit_offsets(hd):
     assert float(hd.grad_clip([t], 6.5)) == 13.0
     assert [float(t[i]) for i in (0, 1 << 30, n - 1)] == [1.5, 2.0, 6.0]
     assert float(hd.grad_norm([t])) == 6.5
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("N", [2, 200])
+@pytest.mark.parametrize("size", [3.0, 100.0, 333.0, 4000.0, 50000.0])
+def test_gradients_of_far_scores_are_whole(hd, N, size, dtype):
+    """Two classes' scores at 32 size and its opposite, all others' at zero: the probability of the first is one and of all others
+    zero (e^-96 and less), so rows whose target it is have no gradient at all and the others' is a difference of two
+    weights.  The scores, and so their difference from lse, are exact."""
+    if dtype == torch.float16 and size > 4000:
+        pytest.skip("beyond the type")
+    size = float(torch.tensor(size).to(dtype))
+    w = torch.zeros(130, 8, device="cuda", dtype=dtype)
+    w[7, 0], w[9, 0] = 32.0, -32.0
+    x = torch.zeros(N, 8, device="cuda", dtype=dtype)
+    x[:, 0] = size
+    tokens = torch.full((N,), 7, dtype=torch.int64, device="cuda")
+    tokens[1::2] = 9
+    _, lse = hd.xent_fprop(x, w, tokens)
+    assert bool((lse == 32 * size).all())
+    gx, gw = hd.xent_backward(x, w, tokens, lse)
+    assert float(gx[0::2].abs().max()) == 0 and bool((gx[1::2, 0] == 64.0).all()) and float(gx[:, 1:].abs().max()) == 0
+    odd = float(torch.tensor(size * (N // 2)).to(dtype))
+    assert float(gw[7, 0]) == odd and float(gw[9, 0]) == -odd
+    gw[[7, 9]] = 0
+    assert float(gw.abs().max()) == 0
